@@ -77,6 +77,14 @@ extern "C" {
 #define ASTRAEA_VARIANT_SELECT_QK   1        /* as above, with the self-attention also restricted to the selected keys / values */
 #define ASTRAEA_VARIANT_TIMESTEP    2        /* Timestep-level: a step computes all tokens or none (budgets must be 0 or N_sel) */
 #define ASTRAEA_VARIANT_FIXED_TOKEN 3        /* Fixed-token: block 0 selects, the other blocks of the step reuse its selection */
+/* flags of astraea_head_rows */
+#define ASTRAEA_ROWS_COMPACT_IN   1u         /* x holds the listed rows only: its row r is the row of token idx[b,r] */
+#define ASTRAEA_ROWS_COMPACT_OUT  2u         /* so does y */
+/* norm and rotation of astraea_qk_norm_rotate */
+#define ASTRAEA_NORM_RMS          0          /* z = x / sqrt(mean x^2 + eps) * weight */
+#define ASTRAEA_NORM_LAYER        1          /* z = (x - mean) / sqrt(var + eps) * weight + bias */
+#define ASTRAEA_ROTATE_INTERLEAVED 0         /* pair p is channels (2p, 2p + 1) */
+#define ASTRAEA_ROTATE_HALF       1          /* pair p is channels (p, p + d/2) */
 /* flags of astraea_scatter_reuse */
 #define ASTRAEA_SCATTER_SRC_FULL  1u         /* rows is [B,N,row_elems]; row idx[r] of it is copied to row idx[r] of cache */
 
@@ -87,6 +95,9 @@ extern "C" {
 #define ASTRAEA_OP_SPARSE_ATTN_KV 4          /* astraea_sparse_attn with kv_idx: pass M_kv as the M argument */
 #define ASTRAEA_OP_GATHERED_LINEAR 5        /* astraea_gathered_linear (the size arguments are ignored) */
 #define ASTRAEA_OP_LAYERNORM    6            /* astraea_layernorm_modulate (the size arguments are ignored) */
+#define ASTRAEA_OP_QK_NORM_ROTATE 7          /* astraea_qk_norm_rotate (the size arguments are ignored) */
+#define ASTRAEA_OP_QUANTIZE_FP8 8            /* astraea_quantize_fp8 (the size arguments are ignored) */
+#define ASTRAEA_OP_GATHERED_LINEAR_FP8 9     /* astraea_gathered_linear_fp8 (the size arguments are ignored) */
 
 /*
  * Selection metric (Section 3.2 "Selection Metric"; Algorithm 1 lines 1-2):
@@ -321,6 +332,75 @@ int32_t astraea_gathered_linear_residual(const void *x, const int32_t *idx, int 
 int32_t astraea_layernorm_modulate(const void *x, const int32_t *idx, int M, const void *scale, const void *shift,
                                    void *y, int B, int N, int D, float eps, uint32_t flags,
                                    void *err_workspace, void *stream);
+
+/*
+ * Norms of queries and keys for each head and the rotation by position, in one pass over the rows: what a block that has
+ * them does between its projections and its attention (a layer that acts on every token by itself, Section 3.2: the
+ * queries of the selected tokens only, the keys of all).  For every listed token i and head h, with z = norm(x[b,i,h,:]),
+ *     y[b,i,h,c]  = z[c] cos[i,p] - z[c'] sin[i,p]
+ *     y[b,i,h,c'] = z[c] sin[i,p] + z[c'] cos[i,p]         for the pairs p = (c, c') of `rotation`
+ * Tokens n_rot and above (text behind the latent) are normalised and not rotated.
+ *   rows   : HOST array of n = 1 or 2 tensors (queries and keys, each with heads, lists and weights of its own) that go in
+ *            one launch:
+ *              x, y    bf16 heads, head_dim contiguous; element strides (batch, head, token) given per tensor, multiples of
+ *                      8.  y may be x (with the same strides and both or neither compact); other overlaps are not allowed.
+ *              idx, M  int32 [B, M] strictly ascending in [0, N); NULL => all N rows (M ignored, no compact flags)
+ *              H       heads
+ *              weight, bias  bf16 [d], shared by the heads; NULL => ones / zeros (bias with the layer norm only)
+ *              flags   ASTRAEA_ROWS_COMPACT_*: with COMPACT_IN alone new rows go to their places in a cache of N tokens
+ *   cos, sin : fp32 [n_rot, d/2], the row of token i for i < n_rot; NULL with n_rot = 0
+ *   err_workspace : NULL, or any workspace of this library: bad index entries are skipped and then reported there
+ * The rows of y that are not listed are left as they were.  fp32 arithmetic, one rounding to bf16.  head_dim 64, 72, 128.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim, unknown norm, rotation or flag), CUDA.
+ */
+typedef struct astraea_head_rows {
+    const void *x;
+    int64_t x_sb, x_sh, x_sn;
+    void *y;
+    int64_t y_sb, y_sh, y_sn;
+    const int32_t *idx;
+    const void *weight, *bias;
+    int32_t M, H;
+    uint32_t flags;
+} astraea_head_rows;
+int32_t astraea_qk_norm_rotate(const astraea_head_rows *rows, int n, const float *cos, const float *sin, int n_rot,
+                               int B, int N, int d, int norm, int rotation, float eps, void *err_workspace, void *stream);
+
+/*
+ * Operands of a linear layer in 8 bits: e4m3 codes with a scale for each 128 channels,
+ *     scale = max(largest magnitude of the block, 2^-100) / 448,     code = x / scale, rounded to e4m3 (ties to even).
+ * astraea_quantize_fp8: the listed rows of x, a block being 128 channels of a row.
+ *   x       : bf16 [B, N, K] (ASTRAEA_LINEAR_COMPACT_IN: [B, M, K])
+ *   idx     : int32 [B, M] strictly ascending in [0, N); NULL => all N rows (M ignored)
+ *   xq      : out e4m3 [B, M, K]           x_scale : out fp32 [K / 128, B * M] (a block's scales of all rows side by side)
+ *   err_workspace : as above; the codes and scales of a row with a bad entry are left as they were
+ * astraea_quantize_fp8_weight: a matrix w bf16 [N_out, K], a block being 128 rows x 128 columns (fewer rows in the last).
+ *   wq      : out e4m3 [N_out, K]          w_scale : out fp32 [ceil(N_out / 128), K / 128]
+ * K a multiple of 128, pointers 16-byte aligned (scales 4).  A NaN stays a NaN in its place and does not count for the scale; a
+ * block that holds an infinity has an infinite scale, and all its values are then NaN.
+ * Errors: INVALID_ARG, UNSUPPORTED (unknown flags), CUDA.
+ */
+int32_t astraea_quantize_fp8(const void *x, const int32_t *idx, int M, void *xq, float *x_scale, int B, int N, int K,
+                             uint32_t flags, void *err_workspace, void *stream);
+int32_t astraea_quantize_fp8_weight(const void *w, void *wq, float *w_scale, int N_out, int K, void *stream);
+
+/*
+ * astraea_gathered_linear_residual on such operands:
+ *     y[b, idx[b,r], n] = residual[b, idx[b,r], n] + gate[b, n] * act(bias[n] + sum over blocks kb of 128 channels of
+ *                         x_scale[kb, b M + r] w_scale[n / 128, kb] (xq[b, r, kb] . wq[n, kb]))
+ *   xq, x_scale, wq, w_scale : as astraea_quantize_fp8(_weight) leaves them; xq holds the listed rows only
+ *   idx, M   : where the rows of xq go (NULL: xq has all N rows of every batch element)
+ *   bias, residual, gate : bf16, each may be NULL; y : bf16 [B, N, N_out], rows at idx written in place
+ *   flags    : ASTRAEA_LINEAR_COMPACT_OUT, _GELU, _COMPACT_RES as there (COMPACT_IN has nothing to say: xq is always compact)
+ *   workspace : at least 256 bytes, 256-byte aligned, zero before the first use (the error word)
+ * Products of a block exact, summed in fp32 by the tensor cores; scaled and summed over the blocks in fp32; one rounding to
+ * bf16.  K a multiple of 128, N_out of 8; pointers 16-byte aligned (scales 4).  M = 0 is valid.  Bad index entries as there.
+ * Errors: INVALID_ARG, UNSUPPORTED (unknown flags), WORKSPACE_TOO_SMALL, CUDA.
+ */
+int32_t astraea_gathered_linear_fp8(const void *xq, const float *x_scale, const int32_t *idx, int M,
+                                    const void *wq, const float *w_scale, const void *bias, const void *residual, const void *gate,
+                                    void *y, int B, int N, int K, int N_out, uint32_t flags,
+                                    void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * One whole compute block (self-attention, cross-attention, MLP; pre-norm, residual) at one denoising step with

@@ -26,14 +26,19 @@ SCATTER_SRC_FULL = 1
 LINEAR_COMPACT_OUT, LINEAR_COMPACT_IN, LINEAR_GELU, LINEAR_COMPACT_RES = 1, 2, 4, 8
 LN_COMPACT_IN, LN_COMPACT_OUT = 1, 2
 BLOCK_REUSE_SELECTION, BLOCK_SELECT_QK = 1, 2
+ROWS_COMPACT_IN, ROWS_COMPACT_OUT = 1, 2
+NORM_RMS, NORM_LAYER = 0, 1
+ROTATE_INTERLEAVED, ROTATE_HALF = 0, 1
 VARIANT_TOKEN_WISE, VARIANT_SELECT_QK, VARIANT_TIMESTEP, VARIANT_FIXED_TOKEN = 0, 1, 2, 3
 OP_SELECT, OP_SPARSE_ATTN, OP_STEP, OP_SPARSE_ATTN_KV, OP_GATHERED_LINEAR, OP_LAYERNORM = 1, 2, 3, 4, 5, 6
+OP_QK_NORM_ROTATE, OP_QUANTIZE_FP8, OP_GATHERED_LINEAR_FP8 = 7, 8, 9
 N_SKIP_CLAMP = 80
 NOALLOC_SCRATCH_BYTES = 4096
 
 EXPORTS = [
     "astraea_score", "astraea_score_partial", "astraea_score_combine", "astraea_select", "astraea_sparse_attn", "astraea_sparse_attn_plan", "astraea_sparse_cross_attn", "astraea_sparse_attn_noalloc", "astraea_scatter_reuse", "astraea_step",
     "astraea_gathered_linear", "astraea_gathered_linear_residual", "astraea_layernorm_modulate",
+    "astraea_qk_norm_rotate", "astraea_quantize_fp8", "astraea_quantize_fp8_weight", "astraea_gathered_linear_fp8",
     "astraea_block_step", "astraea_block_workspace_bytes", "astraea_model_schedule_create", "astraea_model_schedule_launch",
     "astraea_model_schedule_destroy", "astraea_timestep_level_budgets", "astraea_schedule_create", "astraea_schedule_launch", "astraea_schedule_destroy",
     "astraea_session_create", "astraea_session_destroy", "astraea_step_host", "astraea_session_last_h2d_bytes",
@@ -52,6 +57,14 @@ class BlockWeights(ctypes.Structure):
 class BlockState(ctypes.Structure):
     """struct astraea_block_state: the cross-step state of one compute block."""
     _fields_ = [("x_ref", ctypes.c_void_p), ("lse_cache", ctypes.c_void_p), ("n_skip", ctypes.c_void_p), ("y_cache", ctypes.c_void_p)]
+
+
+class HeadRows(ctypes.Structure):
+    """struct astraea_head_rows: one tensor of astraea_qk_norm_rotate (see head_rows)."""
+    _fields_ = [("x", ctypes.c_void_p), ("x_sb", ctypes.c_int64), ("x_sh", ctypes.c_int64), ("x_sn", ctypes.c_int64),
+                ("y", ctypes.c_void_p), ("y_sb", ctypes.c_int64), ("y_sh", ctypes.c_int64), ("y_sn", ctypes.c_int64),
+                ("idx", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("M", ctypes.c_int32), ("H", ctypes.c_int32), ("flags", ctypes.c_uint32)]
 
 
 class AstraeaError(RuntimeError):
@@ -89,6 +102,10 @@ def lib() -> ctypes.CDLL:
         L.astraea_gathered_linear.argtypes = [c_p, c_p, c_i, c_p, c_p, c_p, c_i, c_i, c_i, c_i, c_u, c_p, c_sz, c_p]
         L.astraea_gathered_linear_residual.argtypes = [c_p, c_p, c_i, c_p, c_p, c_p, c_p, c_p, c_i, c_i, c_i, c_i, c_u, c_p, c_sz, c_p]
         L.astraea_layernorm_modulate.argtypes = [c_p, c_p, c_i, c_p, c_p, c_p, c_i, c_i, c_i, c_f, c_u, c_p, c_p]
+        L.astraea_qk_norm_rotate.argtypes = [ctypes.POINTER(HeadRows), c_i, c_p, c_p] + [c_i] * 6 + [c_f, c_p, c_p]
+        L.astraea_quantize_fp8.argtypes = [c_p, c_p, c_i, c_p, c_p, c_i, c_i, c_i, c_u, c_p, c_p]
+        L.astraea_quantize_fp8_weight.argtypes = [c_p, c_p, c_p, c_i, c_i, c_p]
+        L.astraea_gathered_linear_fp8.argtypes = [c_p, c_p, c_p, c_i] + [c_p] * 6 + [c_i, c_i, c_i, c_i, c_u, c_p, c_sz, c_p]
         L.astraea_block_step.argtypes = [c_p, ctypes.POINTER(BlockWeights), ctypes.POINTER(BlockState), c_p, c_p, c_i, c_p, c_p, c_p,
                                          c_i, c_i, c_i, c_i, c_i, c_i, c_f, c_f, c_i, c_i, c_f, c_u, c_p, c_sz, c_p]
         L.astraea_model_schedule_create.argtypes = [ctypes.POINTER(c_p), c_i, c_i, c_p, c_p, ctypes.POINTER(BlockWeights),
@@ -121,7 +138,8 @@ def lib() -> ctypes.CDLL:
         L.astraea_last_error.restype = ctypes.c_char_p
         L.astraea_version.restype = ctypes.c_char_p
         for name in ("astraea_score", "astraea_select", "astraea_sparse_attn", "astraea_sparse_cross_attn", "astraea_sparse_attn_noalloc", "astraea_scatter_reuse",
-                     "astraea_step", "astraea_gathered_linear", "astraea_gathered_linear_residual", "astraea_layernorm_modulate", "astraea_block_step", "astraea_model_schedule_create", "astraea_model_schedule_launch",
+                     "astraea_step", "astraea_gathered_linear", "astraea_gathered_linear_residual", "astraea_layernorm_modulate", "astraea_qk_norm_rotate", "astraea_quantize_fp8",
+                     "astraea_quantize_fp8_weight", "astraea_gathered_linear_fp8", "astraea_block_step", "astraea_model_schedule_create", "astraea_model_schedule_launch",
                      "astraea_timestep_level_budgets", "astraea_schedule_create", "astraea_schedule_launch",
                      "astraea_session_create", "astraea_step_host", "astraea_budget_to_k",
                      "astraea_poll_error"):
@@ -259,6 +277,41 @@ def astraea_layernorm_modulate(x, idx, M, scale, shift, y, B, N, D, eps=1e-6, fl
         return
     _check(lib().astraea_layernorm_modulate(_ptr(x), _ptr(idx), M, _ptr(scale), _ptr(shift), _ptr(y), B, N, D, eps, flags,
                                             _ptr(workspace), _stream(stream)))
+
+
+def head_rows(x, x_strides, y, y_strides, H, idx=None, M=0, weight=None, bias=None, flags=0) -> HeadRows:
+    """One tensor of astraea_qk_norm_rotate; strides are (batch, head, token) element strides.  The caller keeps the tensors alive
+    until the call has been made."""
+    # (an empty index tensor has a null data pointer, which the C ABI reads as "all rows": any other address will do, nothing reads it)
+    lst = None if idx is None else (idx.data_ptr() or 1)
+    return HeadRows(_ptr(x), *x_strides, _ptr(y), *y_strides, lst, _ptr(weight), _ptr(bias), M, H, flags)
+
+
+def astraea_qk_norm_rotate(rows, cos, sin, n_rot, B, N, d, norm=NORM_RMS, rotation=ROTATE_INTERLEAVED, eps=1e-6, workspace=None, stream=None) -> None:
+    """Per-head norm and rotation by position of one or two tensors (a list of head_rows(...)): queries and keys in one launch."""
+    _check(lib().astraea_qk_norm_rotate((HeadRows * len(rows))(*rows), len(rows), _ptr(cos), _ptr(sin), n_rot, B, N, d, norm, rotation, eps,
+                                        _ptr(workspace), _stream(stream)))
+
+
+def astraea_quantize_fp8(x, idx, M, xq, x_scale, B, N, K, flags=0, workspace=None, stream=None) -> None:
+    """The listed rows of x (idx None: all) as e4m3 [B, M, K] with scales fp32 [K / 128, B * M]."""
+    if idx is not None and M == 0:
+        return
+    _check(lib().astraea_quantize_fp8(_ptr(x), _ptr(idx), M, _ptr(xq), _ptr(x_scale), B, N, K, flags, _ptr(workspace), _stream(stream)))
+
+
+def astraea_quantize_fp8_weight(w, wq, w_scale, N_out, K, stream=None) -> None:
+    """A weight matrix as e4m3 [N_out, K] with scales fp32 [ceil(N_out / 128), K / 128]."""
+    _check(lib().astraea_quantize_fp8_weight(_ptr(w), _ptr(wq), _ptr(w_scale), N_out, K, _stream(stream)))
+
+
+def astraea_gathered_linear_fp8(xq, x_scale, idx, M, wq, w_scale, bias, residual, gate, y, B, N, K, N_out, flags=0, workspace=None, stream=None) -> None:
+    """y[rows] = residual[rows] + gate[b] * act(x @ w.T + bias) on operands as the two quantisers leave them (xq holds the listed rows)."""
+    if idx is not None and M == 0:
+        return
+    _check(lib().astraea_gathered_linear_fp8(_ptr(xq), _ptr(x_scale), _ptr(idx), M, _ptr(wq), _ptr(w_scale), _ptr(bias), _ptr(residual), _ptr(gate),
+                                             _ptr(y), B, N, K, N_out, flags, _ptr(workspace),
+                                             workspace.numel() if workspace is not None else 0, _stream(stream)))
 
 
 def astraea_block_workspace_bytes(B: int, H: int, N: int, d: int, hidden: int) -> int:

@@ -126,6 +126,15 @@ int32_t launch_gathered_linear(const void *x, const int32_t *idx, int M, const L
 int32_t launch_layernorm_modulate(const void *x, const int32_t *idx, int M, const void *scale, const void *shift, void *y,
                                   int B, int N, int D, float eps, uint32_t flags, int *err_word, cudaStream_t stream);
 
+int32_t launch_qk_norm_rotate(const astraea_head_rows *rows, int n, const float *cos, const float *sin, int n_rot, int B, int N, int d,
+                              bool layer, bool half, float eps, int *err_word, cudaStream_t stream);
+int32_t launch_quantize_fp8(const void *x, const int32_t *idx, int M, void *xq, float *x_scale, int B, int N, int K, bool compact_in,
+                            int *err_word, cudaStream_t stream);
+int32_t launch_quantize_fp8_weight(const void *w, void *wq, float *w_scale, int N_out, int K, cudaStream_t stream);
+int32_t launch_gathered_linear_fp8(const void *xq, const float *x_scale, const int32_t *idx, int M, const void *wq, const float *w_scale,
+                                   const void *bias, const void *residual, const void *gate, void *y, int B, int N, int K, int N_out,
+                                   uint32_t flags, int *err_word, cudaStream_t stream);
+
 struct AttnArgs {
     const void *q, *k, *v;
     int64_t q_sb, q_sh, q_sn, k_sb, k_sh, k_sn, v_sb, v_sh, v_sn;

@@ -1,0 +1,271 @@
+// astraea_qk_norm_rotate: every head of the listed rows of a tensor of heads (queries, keys) is normalised over its d channels and
+// rotated by the position of its token,
+//     z = norm(x[b, i, h, :]) * weight + bias,   y[b, i, h, (p, p')] = (z_p cos_i,p - z_p' sin_i,p,  z_p sin_i,p + z_p' cos_i,p),
+// what a block that normalises its queries and keys and encodes positions by rotation does between its projections and its attention
+// (Section 3.2: such layers act on every token by itself, so queries are needed for the selected tokens only; keys for all).
+//
+// HBM-bound: every value is read once and written once, in one launch for queries and keys.  A warp takes one token's heads (a share of
+// them in short launches); its cosines and sines, 4 d bytes, are read once for all of them, weights once per warp.  A lane owns the same
+// piece of the first and of the second half of a head (16 bytes each; 8 at head_dim 72, whose halves are 72 bytes), so that both ways of
+// pairing channels, (2p, 2p + 1) and (p, p + d/2), stay inside a lane and only the sums of the norm go round: over 4, 9 or 8 lanes.
+// fp32 arithmetic, one rounding to bf16 at the end.
+#include "common.cuh"
+
+namespace astraea {
+namespace {
+
+constexpr int kWarps = 4;                                          // per block
+constexpr int kUnroll = 3;                                         // heads in flight per lane: divides the steps of 24 x 128, 16 x 72, 48 x 64
+
+struct HeadTensor {
+    const __nv_bfloat16 *x;
+    __nv_bfloat16 *y;
+    int64_t x_sb, x_sh, x_sn, y_sb, y_sh, y_sn;
+    const int32_t *idx;
+    const __nv_bfloat16 *weight, *bias;
+    int M, H, compact_in, compact_out;
+    int parts, part_heads;                                         // a token's heads are shared out over `parts` warps
+};
+struct HeadNormParams {
+    HeadTensor t[2];
+    int units0, units;                                             // of t[0], of both: B * M * parts each
+    const float *cos, *sin;
+    int n_rot, N;
+    float eps;
+    int *err_word;
+};
+
+template <int DH> struct Lanes {
+    static constexpr int kPiece = DH == 72 ? 4 : 8;                // channels of a lane's piece of each half
+    static constexpr int kGroup = DH / 2 / kPiece;                 // lanes of a head: 4, 9, 8
+    static constexpr int kHeads = 32 / kGroup;                     // heads that a warp takes at once: 8, 3, 4
+};
+
+// one piece of a head: 16 or 8 bytes
+template <int P> __device__ __forceinline__ void load_piece(const __nv_bfloat16 *p, uint32_t (&r)[P / 2]) {
+    if constexpr (P == 8) {
+        const uint4 v = ld_stream(reinterpret_cast<const uint4 *>(p));
+        r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
+    } else asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
+}
+template <int P> __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const f32x2 (&f)[P / 2]) {
+    uint32_t w[P / 2];
+#pragma unroll
+    for (int i = 0; i < P / 2; ++i) {
+        float lo, hi;
+        unpack2(f[i], lo, hi);
+        __nv_bfloat162 v2 = __floats2bfloat162_rn(lo, hi);
+        w[i] = *reinterpret_cast<uint32_t *>(&v2);
+    }
+    if constexpr (P == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+}
+__device__ __forceinline__ f32x2 widen(uint32_t w) { return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ f32x2 twice(float v) { return pack2(v, v); }
+
+// the sum over the lanes of a head
+template <int G> __device__ __forceinline__ float group_sum(float s, int lane) {
+    if constexpr (G == 9) {
+        const int base = lane / 9 * 9, l = lane - base;            // lanes 27..31 hold no head: their sums are not used
+        const float t = s + __shfl_sync(0xffffffffu, s, base + (l + 3) % 9) + __shfl_sync(0xffffffffu, s, base + (l + 6) % 9);
+        return t + __shfl_sync(0xffffffffu, t, base + (l + 1) % 9) + __shfl_sync(0xffffffffu, t, base + (l + 2) % 9);
+    } else {
+#pragma unroll
+        for (int o = G / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        return s;
+    }
+}
+
+// LAYER: layer norm with a bias (RMS norm without one otherwise); HALF: channels are paired (p, p + DH/2) and not (2p, 2p + 1)
+template <int DH, bool LAYER, bool HALF>
+__global__ void __launch_bounds__(kWarps * 32) head_norm_kernel(const __grid_constant__ HeadNormParams p)
+{
+    using L = Lanes<DH>;
+    constexpr int P = L::kPiece, G = L::kGroup, kPairs = P / 2;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int sub = lane / G, l = lane - sub * G;                  // head of the warp's kHeads, piece of the head
+    const bool on = sub < L::kHeads;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    int held = -1;                                                 // tensor whose weights are held
+    f32x2 w[2][kPairs], bi[2][LAYER ? kPairs : 1];
+    for (int u = blockIdx.x * kWarps + warp; u < p.units; u += gridDim.x * kWarps) {
+        const int which = u >= p.units0 ? 1 : 0;
+        const HeadTensor &t = p.t[which];
+        const int v = which ? u - p.units0 : u;
+        const int row = t.parts == 1 ? v : v / t.parts, part = v - row * t.parts;
+        const int b = row / t.M, r = row - b * t.M;
+        const int tok = t.idx ? __ldcg(t.idx + row) : r;
+        const int before = (t.idx && r > 0) ? __ldcg(t.idx + row - 1) : -1;
+        if ((unsigned)tok >= (unsigned)p.N || before >= tok) {     // see astraea_scatter_reuse
+            if (lane == 0 && part == 0 && p.err_word) atomicExch(p.err_word, kErrBadIndex);
+            continue;
+        }
+        if (which != held) {
+            held = which;
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    const int c = s * (DH / 2) + l * P + 2 * i;
+                    const uint32_t one = 0x3F803F80u;
+                    w[s][i] = widen(on && t.weight ? *reinterpret_cast<const volatile uint32_t *>(t.weight + c) : one);
+                    if (LAYER) bi[s][LAYER ? i : 0] = widen(on && t.bias ? *reinterpret_cast<const volatile uint32_t *>(t.bias + c) : 0u);
+                }
+        }
+        // angles: HALF: of channels l P .. of the first half, as many as the piece has channels; else those of the pairs of both pieces
+        float co[P], si[P];
+        if (on && tok < p.n_rot) {
+            const float *pc = p.cos + (size_t)tok * (DH / 2), *ps = p.sin + (size_t)tok * (DH / 2);
+            auto get = [&](const float *src, float (&dst)[P]) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const float *a = src + (HALF ? l * P + s * kPairs : s * (DH / 4) + l * kPairs);
+                    if constexpr (P == 8) {
+                        float4 f;
+                        asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "l"(a));
+                        dst[s * 4] = f.x; dst[s * 4 + 1] = f.y; dst[s * 4 + 2] = f.z; dst[s * 4 + 3] = f.w;
+                    } else asm volatile("ld.global.v2.f32 {%0,%1}, [%2];" : "=f"(dst[s * 2]), "=f"(dst[s * 2 + 1]) : "l"(a));
+                }
+            };
+            get(pc, co);
+            get(ps, si);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) { co[i] = 1.f; si[i] = 0.f; }
+        }
+        const __nv_bfloat16 *src = t.x + b * t.x_sb + (int64_t)(t.compact_in ? r : tok) * t.x_sn + l * P;
+        __nv_bfloat16 *dst = t.y + b * t.y_sb + (int64_t)(t.compact_out ? r : tok) * t.y_sn + l * P;
+        const int h0 = part * t.part_heads, h1 = min(t.H, h0 + t.part_heads);
+        for (int hb = h0 + sub; hb - sub < h1; hb += kUnroll * L::kHeads) {
+            uint32_t raw[kUnroll][2][kPairs];
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                const int h = hb + k * L::kHeads;
+                if (on && h < h1) {
+                    load_piece<P>(src + h * t.x_sh, raw[k][0]);
+                    load_piece<P>(src + h * t.x_sh + DH / 2, raw[k][1]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) raw[k][0][i] = raw[k][1][i] = 0u;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kUnroll; ++k) {
+                const int h = hb + k * L::kHeads;
+                if (h - sub >= h1) break;                          // the whole warp: no head of this step is left
+                f32x2 z[2][kPairs];
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) z[s][i] = widen(raw[k][s][i]);
+                float lo, hi;
+                if (LAYER) {
+                    f32x2 a = 0ull;
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) a = add2(a, add2(z[0][i], z[1][i]));
+                    unpack2(a, lo, hi);
+                    const f32x2 minus_mean = twice(group_sum<G>(lo + hi, lane) * (-1.0f / DH));
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) z[s][i] = add2(z[s][i], minus_mean);
+                }
+                f32x2 a = 0ull;
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) a = fma2(z[1][i], z[1][i], fma2(z[0][i], z[0][i], a));
+                unpack2(a, lo, hi);
+                const f32x2 rstd = twice(rsqrtf(group_sum<G>(lo + hi, lane) * (1.0f / DH) + p.eps));
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        z[s][i] = mul2(z[s][i], rstd);
+                        z[s][i] = LAYER ? fma2(z[s][i], w[s][i], bi[s][LAYER ? i : 0]) : mul2(z[s][i], w[s][i]);
+                    }
+                if (HALF) {
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        const f32x2 c2 = pack2(co[2 * i], co[2 * i + 1]), s2 = pack2(si[2 * i], si[2 * i + 1]), m2 = pack2(-si[2 * i], -si[2 * i + 1]);
+                        const f32x2 a0 = z[0][i], a1 = z[1][i];
+                        z[0][i] = fma2(a0, c2, mul2(a1, m2));
+                        z[1][i] = fma2(a1, c2, mul2(a0, s2));
+                    }
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) {
+                            unpack2(z[s][i], lo, hi);
+                            const float c = co[s * kPairs + i], n = si[s * kPairs + i];
+                            z[s][i] = fma2(z[s][i], twice(c), mul2(pack2(hi, lo), pack2(-n, n)));
+                        }
+                }
+                if (on && h < h1) {
+                    store_piece<P>(dst + h * t.y_sh, z[0]);
+                    store_piece<P>(dst + h * t.y_sh + DH / 2, z[1]);
+                }
+            }
+        }
+    }
+}
+
+template <int DH>
+int32_t launch_dim(HeadNormParams &p, const astraea_head_rows *rows, int n, int B, bool layer, bool half, cudaStream_t stream)
+{
+    // A token's heads go to one warp where that gives every SM its 32 warps, and are shared out in steps of a warp's heads where it does
+    // not: one token of 32 + 8 heads is then 10 warps and not 2.
+    long long all_rows = 0;
+    for (int i = 0; i < n; ++i) all_rows += (long long)B * p.t[i].M;
+    const long long slots = (long long)sm_count() * 32;
+    long long units[2] = {0, 0};
+    for (int i = 0; i < n; ++i) {
+        HeadTensor &t = p.t[i];
+        const int steps = (t.H + Lanes<DH>::kHeads - 1) / Lanes<DH>::kHeads;
+        long long want = all_rows > 0 ? slots / all_rows : 1;
+        want = want < 1 ? 1 : want > steps ? steps : want;
+        const int part_steps = (int)((steps + want - 1) / want);
+        t.part_heads = part_steps * Lanes<DH>::kHeads;
+        t.parts = (steps + part_steps - 1) / part_steps;
+        units[i] = (long long)B * t.M * t.parts;
+    }
+    if (units[0] + units[1] > 0x3fffffffll) return fail(ASTRAEA_ERR_INVALID_ARG, "astraea_qk_norm_rotate: too many rows");
+    p.units0 = (int)units[0];
+    p.units = (int)(units[0] + units[1]);
+    if (p.units == 0) return ASTRAEA_OK;
+    const long long want = (p.units + kWarps - 1) / kWarps, cap = (long long)sm_count() * 16;
+    const int grid = (int)(want < cap ? want : cap);
+    auto kernel = layer ? (half ? head_norm_kernel<DH, true, true> : head_norm_kernel<DH, true, false>)
+                        : (half ? head_norm_kernel<DH, false, true> : head_norm_kernel<DH, false, false>);
+    launch_overlapped(kernel, grid, kWarps * 32, 0, stream, p);
+    return check_launch("astraea_qk_norm_rotate");
+}
+
+}  // namespace
+
+int32_t launch_qk_norm_rotate(const astraea_head_rows *rows, int n, const float *cos, const float *sin, int n_rot, int B, int N, int d,
+                              bool layer, bool half, float eps, int *err_word, cudaStream_t stream)
+{
+    HeadNormParams p = {};
+    for (int i = 0; i < n; ++i) {
+        HeadTensor &t = p.t[i];
+        const astraea_head_rows &a = rows[i];
+        t.x = reinterpret_cast<const __nv_bfloat16 *>(a.x);
+        t.y = reinterpret_cast<__nv_bfloat16 *>(a.y);
+        t.x_sb = a.x_sb; t.x_sh = a.x_sh; t.x_sn = a.x_sn;
+        t.y_sb = a.y_sb; t.y_sh = a.y_sh; t.y_sn = a.y_sn;
+        t.idx = a.idx; t.M = a.idx ? a.M : N; t.H = a.H;
+        t.weight = reinterpret_cast<const __nv_bfloat16 *>(a.weight);
+        t.bias = reinterpret_cast<const __nv_bfloat16 *>(a.bias);
+        t.compact_in = (a.flags & ASTRAEA_ROWS_COMPACT_IN) ? 1 : 0;
+        t.compact_out = (a.flags & ASTRAEA_ROWS_COMPACT_OUT) ? 1 : 0;
+    }
+    p.cos = cos; p.sin = sin; p.n_rot = n_rot; p.N = N; p.eps = eps; p.err_word = err_word;
+    switch (d) {
+    case 64: return launch_dim<64>(p, rows, n, B, layer, half, stream);
+    case 72: return launch_dim<72>(p, rows, n, B, layer, half, stream);
+    default: return launch_dim<128>(p, rows, n, B, layer, half, stream);
+    }
+}
+
+}  // namespace astraea

@@ -1,0 +1,158 @@
+// astraea_quantize_fp8: the listed rows of x as e4m3 with a scale for each row and 128 channels; astraea_quantize_fp8_weight: a weight
+// matrix as e4m3 with a scale for each block of 128 x 128.  The operands of astraea_gathered_linear_fp8.
+//     scale = max(largest magnitude of the block, 2^-100) / 448,    q = x / scale rounded to e4m3 (ties to even)
+// so that the largest value of a block takes the largest code (448) and the scales of all-zero blocks stay normal numbers.
+//
+// HBM-bound: two bytes in and one out for every value.  A warp takes a row; a block of 128 channels is 16 lanes with 16 bytes each, whose
+// largest magnitude goes round by four shuffles.  Four pairs of blocks are in flight per warp.  The quotient is x * (1 / scale) and one
+// residual step, which is the correctly rounded quotient for all but a few operands; a rounding of its own before the one to e4m3 would
+// decide the many exact ties that bf16 values have (a plain product moves 1 in 300 codes by one).
+#include "common.cuh"
+
+namespace astraea {
+namespace {
+
+constexpr float kE4M3Max = 448.0f, kLeastAmax = 7.888609052210118e-31f;       // 2^-100
+constexpr int kWarps = 8;
+constexpr int kUnroll = 4;
+
+__device__ __forceinline__ uint32_t amax_bits(const uint4 &v) {               // largest magnitude of eight bf16, NaN left out
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    __nv_bfloat162 m = __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[0]));
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __hmax2(m, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i])));
+    const __nv_bfloat16 s = __hmax(m.x, m.y);
+    return (uint32_t)*reinterpret_cast<const uint16_t *>(&s);
+}
+__device__ __forceinline__ float as_float(uint32_t bf16_bits) { return __uint_as_float(bf16_bits << 16); }
+
+struct BlockScale { float scale, inv; };
+__device__ __forceinline__ BlockScale scale_of(float amax) {
+    BlockScale s;
+    s.scale = __fdiv_rn(fmaxf(amax, kLeastAmax), kE4M3Max);
+    s.inv = __frcp_rn(s.scale);
+    return s;
+}
+// eight values as e4m3
+__device__ __forceinline__ uint2 encode8(const uint4 &v, const BlockScale &s) {
+    f32x2 x[4];
+    unpack8(v, x);
+    const f32x2 inv = pack2(s.inv, s.inv), minus = pack2(-s.scale, -s.scale);
+    uint32_t out[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        f32x2 q = mul2(x[i], inv);
+        // (an infinite scale: 0 for what is finite, NaN for what is not, and no residual)
+        if (s.inv != 0.f) q = fma2(fma2(q, minus, x[i]), inv, q);
+        float lo, hi;
+        unpack2(q, lo, hi);
+        uint16_t c;
+        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(c) : "f"(hi), "f"(lo));
+        if (i & 1) out[i >> 1] |= (uint32_t)c << 16; else out[i >> 1] = c;
+    }
+    return make_uint2(out[0], out[1]);
+}
+
+__global__ void __launch_bounds__(kWarps * 32)
+quantize_rows_kernel(const uint4 *__restrict__ x, const int32_t *__restrict__ idx, int M, uint2 *__restrict__ xq, float *__restrict__ scale,
+                     int B, int N, int blocks, int parts, int part_blocks, int compact_in, int *__restrict__ err_word)
+{
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, vecs = blocks * 16;
+    const long long rows = (long long)B * M, units = rows * parts;
+    // neighbouring warps take neighbouring rows: the scales of a block of channels lie side by side by row
+    for (long long u = (long long)blockIdx.x * kWarps + warp; u < units; u += (long long)gridDim.x * kWarps) {
+        const int part = (int)(u / rows);
+        const long long t = u - part * rows;
+        const int b = (int)(t / M), r = (int)(t - (long long)b * M);
+        const int tok = idx ? __ldcg(idx + t) : r;
+        const int before = (idx && r > 0) ? __ldcg(idx + t - 1) : -1;
+        const bool bad = (unsigned)tok >= (unsigned)N || before >= tok;
+        if (bad && lane == 0 && part == 0 && err_word) atomicExch(err_word, kErrBadIndex);
+        if (bad) continue;                                          // its row of codes and scales is left as it was
+        const uint4 *src = x + (compact_in ? t : (long long)b * N + tok) * vecs;
+        uint2 *dst = xq + t * vecs;
+        const int k0 = part * part_blocks, k1 = min(blocks, k0 + part_blocks);
+        for (int kb = k0; kb < k1; kb += 2 * kUnroll) {
+            uint4 v[kUnroll];
+#pragma unroll
+            for (int i = 0; i < kUnroll; ++i) {
+                const int c = (kb + 2 * i) * 16 + lane;
+                v[i] = c < k1 * 16 ? ld_stream(src + c) : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < kUnroll; ++i) {
+                const int c = (kb + 2 * i) * 16 + lane;
+                float m = as_float(amax_bits(v[i]));
+#pragma unroll
+                for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const BlockScale s = scale_of(m);
+                if (c < k1 * 16) {
+                    dst[c] = encode8(v[i], s);
+                    if ((lane & 15) == 0) scale[(long long)(c >> 4) * rows + t] = s.scale;
+                }
+            }
+        }
+    }
+}
+
+// one CTA per block of 128 x 128: 256 threads, eight 16-byte vectors each
+__global__ void __launch_bounds__(256)
+quantize_weight_kernel(const uint4 *__restrict__ w, uint2 *__restrict__ wq, float *__restrict__ scale, int N_out, int blocks)
+{
+    __shared__ float part[8];
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int kb = blockIdx.x, nb = blockIdx.y, lane = threadIdx.x & 31, c = threadIdx.x & 15, r0 = threadIdx.x >> 4;
+    uint4 v[8];
+    float m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = nb * 128 + r0 + 16 * i;
+        v[i] = row < N_out ? ld_stream(w + ((long long)row * blocks + kb) * 16 + c) : make_uint4(0, 0, 0, 0);
+        m = fmaxf(m, as_float(amax_bits(v[i])));
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) part[threadIdx.x >> 5] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = fmaxf(m, part[i]);
+    const BlockScale s = scale_of(m);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = nb * 128 + r0 + 16 * i;
+        if (row < N_out) wq[((long long)row * blocks + kb) * 16 + c] = encode8(v[i], s);
+    }
+    if (threadIdx.x == 0) scale[(long long)nb * blocks + kb] = s.scale;
+}
+
+}  // namespace
+
+int32_t launch_quantize_fp8(const void *x, const int32_t *idx, int M, void *xq, float *x_scale, int B, int N, int K, bool compact_in,
+                            int *err_word, cudaStream_t stream)
+{
+    const int rows_each = idx ? M : N, blocks = K / 128;
+    const long long rows = (long long)B * rows_each;
+    if (rows == 0) return ASTRAEA_OK;
+    // A row is one warp's, but in short launches its blocks are shared out over warps, a pair of blocks at least
+    const long long slots = (long long)sm_count() * 32;
+    const int pairs = (blocks + 1) / 2;
+    long long want = slots / rows;
+    want = want < 1 ? 1 : want > pairs ? pairs : want;
+    const int part_blocks = (int)((pairs + want - 1) / want) * 2, parts = (blocks + part_blocks - 1) / part_blocks;
+    const long long ctas = (rows * parts + kWarps - 1) / kWarps, cap = (long long)sm_count() * 8;
+    launch_overlapped(quantize_rows_kernel, (int)(ctas < cap ? ctas : cap), kWarps * 32, 0, stream, reinterpret_cast<const uint4 *>(x), idx, rows_each,
+                      reinterpret_cast<uint2 *>(xq), x_scale, B, N, blocks, parts, part_blocks, compact_in ? 1 : 0, err_word);
+    return check_launch("astraea_quantize_fp8");
+}
+
+int32_t launch_quantize_fp8_weight(const void *w, void *wq, float *w_scale, int N_out, int K, cudaStream_t stream)
+{
+    launch_overlapped(quantize_weight_kernel, dim3(K / 128, (N_out + 127) / 128), 256, 0, stream, reinterpret_cast<const uint4 *>(w),
+                      reinterpret_cast<uint2 *>(wq), w_scale, N_out, K / 128);
+    return check_launch("astraea_quantize_fp8_weight");
+}
+
+}  // namespace astraea
