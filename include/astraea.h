@@ -58,6 +58,7 @@ extern "C" {
                                               * launch-time estimate says (without the flag the library picks the faster shape) */
 #define ASTRAEA_ATTN_WHOLE_KEYS   4u         /* every CTA runs over all keys: the last, partial round of CTAs is never split by keys
                                               * (see `workspace` of astraea_sparse_attn) */
+#define ASTRAEA_ATTN_COMPACT_Q    8u         /* astraea_window_attn: q is [B,M,H,d] (row r of the index list), by the same strides */
 /* flags of astraea_gathered_linear */
 #define ASTRAEA_LINEAR_COMPACT_OUT 1u        /* y is [B,M,N_out] (row r of the index list), not the cache [B,N,N_out] */
 #define ASTRAEA_LINEAR_COMPACT_IN  2u        /* x is [B,M,K]: row r is the row of token idx[b,r] (output of a layer run with COMPACT_OUT) */
@@ -95,6 +96,7 @@ extern "C" {
 #define ASTRAEA_OP_SPARSE_ATTN_KV 4          /* astraea_sparse_attn with kv_idx: pass M_kv as the M argument */
 #define ASTRAEA_OP_GATHERED_LINEAR 5        /* astraea_gathered_linear (the size arguments are ignored) */
 #define ASTRAEA_OP_LAYERNORM    6            /* astraea_layernorm_modulate (the size arguments are ignored) */
+#define ASTRAEA_OP_WINDOW_ATTN 10            /* astraea_window_attn */
 #define ASTRAEA_OP_QK_NORM_ROTATE 7          /* astraea_qk_norm_rotate (the size arguments are ignored) */
 #define ASTRAEA_OP_QUANTIZE_FP8 8            /* astraea_quantize_fp8 (the size arguments are ignored) */
 #define ASTRAEA_OP_GATHERED_LINEAR_FP8 9     /* astraea_gathered_linear_fp8 (the size arguments are ignored) */
@@ -225,6 +227,34 @@ int32_t astraea_sparse_cross_attn(const void *q, const void *k, const void *v,
                                   const int32_t *q_idx, int M, void *out, float *lse_out,
                                   int B, int H, int N, int N_kv, int d, float scale, uint32_t flags,
                                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Attention over a window of keys, for videos that are too long for attention over all of them or that are generated as a
+ * stream: as astraea_sparse_attn, but the query of token p = idx[b,r] sees key j only
+ *     if j < kv_len[b]  and  (j < n_first  or  j >= N - n_last  or  p - left <= j <= p + right),
+ * that is the keys around it, a few first ones (sinks: the first frame) and a few last ones (the always-kept tokens).
+ * right = 0 is causal; left and right of N or more do not bound.  H query heads share H_kv key / value heads: query head h
+ * uses key head h / (H / H_kv).
+ *   q       : bf16 [B, N, H, d] through its strides; with ASTRAEA_ATTN_COMPACT_Q [B, M, H, d]: the listed rows only (a
+ *             stream's newest token against its cache: M = 1, q_idx its place, COMPACT_Q | COMPACT_OUT)
+ *   k, v    : bf16 [B, N, H_kv, d] through their strides; keys that a row does not see, those from kv_len[b] on in
+ *             particular, may hold anything, NaN included
+ *   q_idx, M, out, lse_out, scale, flags : as astraea_sparse_attn (no SMALL_CTAS); N at most 2^30
+ *   kv_len  : int32 [B] keys that exist (values outside [0, N] count as the nearer end); NULL => N
+ *   workspace : 256-byte aligned, at least 256 bytes; with astraea_workspace_bytes(ASTRAEA_OP_WINDOW_ATTN, B, H, N, M, d) the
+ *             units of a last, partial round (all units of a small call) may be shared out by keys over 2..16 CTAs each.  A
+ *             workspace serves one call at a time.
+ * A row that sees no key is 0 and its lse -inf.  Arithmetic and non-finite logits as astraea_sparse_attn (row sums in
+ * fp32 at every head_dim); a value of NaN or infinity reaches the rows that see it, in its channels, and no other.
+ * M = 0 is valid.  Errors: INVALID_ARG, UNSUPPORTED (head_dim, flags), WORKSPACE_TOO_SMALL, CUDA.
+ */
+int32_t astraea_window_attn(const void *q, const void *k, const void *v,
+                            int64_t q_sb, int64_t q_sh, int64_t q_sn,
+                            int64_t k_sb, int64_t k_sh, int64_t k_sn,
+                            int64_t v_sb, int64_t v_sh, int64_t v_sn,
+                            const int32_t *q_idx, int M, const int32_t *kv_len, void *out, float *lse_out,
+                            int B, int H, int H_kv, int N, int d, int n_first, int n_last, int left, int right,
+                            float scale, uint32_t flags, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * The same attention for callers that must not allocate.  (The paper has no counterpart: this is a

@@ -22,6 +22,7 @@ LSE_SUM_EXP, LSE_LOG = 0, 1
 ATTN_COMPACT_OUT = 1
 ATTN_SMALL_CTAS = 2
 ATTN_WHOLE_KEYS = 4
+ATTN_COMPACT_Q = 8
 SCATTER_SRC_FULL = 1
 LINEAR_COMPACT_OUT, LINEAR_COMPACT_IN, LINEAR_GELU, LINEAR_COMPACT_RES = 1, 2, 4, 8
 LN_COMPACT_IN, LN_COMPACT_OUT = 1, 2
@@ -31,14 +32,14 @@ NORM_RMS, NORM_LAYER = 0, 1
 ROTATE_INTERLEAVED, ROTATE_HALF = 0, 1
 VARIANT_TOKEN_WISE, VARIANT_SELECT_QK, VARIANT_TIMESTEP, VARIANT_FIXED_TOKEN = 0, 1, 2, 3
 OP_SELECT, OP_SPARSE_ATTN, OP_STEP, OP_SPARSE_ATTN_KV, OP_GATHERED_LINEAR, OP_LAYERNORM = 1, 2, 3, 4, 5, 6
-OP_QK_NORM_ROTATE, OP_QUANTIZE_FP8, OP_GATHERED_LINEAR_FP8 = 7, 8, 9
+OP_QK_NORM_ROTATE, OP_QUANTIZE_FP8, OP_GATHERED_LINEAR_FP8, OP_WINDOW_ATTN = 7, 8, 9, 10
 N_SKIP_CLAMP = 80
 NOALLOC_SCRATCH_BYTES = 4096
 
 EXPORTS = [
     "astraea_score", "astraea_score_partial", "astraea_score_combine", "astraea_select", "astraea_sparse_attn", "astraea_sparse_attn_plan", "astraea_sparse_cross_attn", "astraea_sparse_attn_noalloc", "astraea_scatter_reuse", "astraea_step",
     "astraea_gathered_linear", "astraea_gathered_linear_residual", "astraea_layernorm_modulate",
-    "astraea_qk_norm_rotate", "astraea_quantize_fp8", "astraea_quantize_fp8_weight", "astraea_gathered_linear_fp8",
+    "astraea_window_attn", "astraea_qk_norm_rotate", "astraea_quantize_fp8", "astraea_quantize_fp8_weight", "astraea_gathered_linear_fp8",
     "astraea_block_step", "astraea_block_workspace_bytes", "astraea_model_schedule_create", "astraea_model_schedule_launch",
     "astraea_model_schedule_destroy", "astraea_timestep_level_budgets", "astraea_schedule_create", "astraea_schedule_launch", "astraea_schedule_destroy",
     "astraea_session_create", "astraea_session_destroy", "astraea_step_host", "astraea_session_last_h2d_bytes",
@@ -102,6 +103,7 @@ def lib() -> ctypes.CDLL:
         L.astraea_gathered_linear.argtypes = [c_p, c_p, c_i, c_p, c_p, c_p, c_i, c_i, c_i, c_i, c_u, c_p, c_sz, c_p]
         L.astraea_gathered_linear_residual.argtypes = [c_p, c_p, c_i, c_p, c_p, c_p, c_p, c_p, c_i, c_i, c_i, c_i, c_u, c_p, c_sz, c_p]
         L.astraea_layernorm_modulate.argtypes = [c_p, c_p, c_i, c_p, c_p, c_p, c_i, c_i, c_i, c_f, c_u, c_p, c_p]
+        L.astraea_window_attn.argtypes = [c_p, c_p, c_p] + [c_i64] * 9 + [c_p, c_i, c_p, c_p, c_p] + [c_i] * 9 + [c_f, c_u, c_p, c_sz, c_p]
         L.astraea_qk_norm_rotate.argtypes = [ctypes.POINTER(HeadRows), c_i, c_p, c_p] + [c_i] * 6 + [c_f, c_p, c_p]
         L.astraea_quantize_fp8.argtypes = [c_p, c_p, c_i, c_p, c_p, c_i, c_i, c_i, c_u, c_p, c_p]
         L.astraea_quantize_fp8_weight.argtypes = [c_p, c_p, c_p, c_i, c_i, c_p]
@@ -138,7 +140,7 @@ def lib() -> ctypes.CDLL:
         L.astraea_last_error.restype = ctypes.c_char_p
         L.astraea_version.restype = ctypes.c_char_p
         for name in ("astraea_score", "astraea_select", "astraea_sparse_attn", "astraea_sparse_cross_attn", "astraea_sparse_attn_noalloc", "astraea_scatter_reuse",
-                     "astraea_step", "astraea_gathered_linear", "astraea_gathered_linear_residual", "astraea_layernorm_modulate", "astraea_qk_norm_rotate", "astraea_quantize_fp8",
+                     "astraea_step", "astraea_gathered_linear", "astraea_gathered_linear_residual", "astraea_layernorm_modulate", "astraea_window_attn", "astraea_qk_norm_rotate", "astraea_quantize_fp8",
                      "astraea_quantize_fp8_weight", "astraea_gathered_linear_fp8", "astraea_block_step", "astraea_model_schedule_create", "astraea_model_schedule_launch",
                      "astraea_timestep_level_budgets", "astraea_schedule_create", "astraea_schedule_launch",
                      "astraea_session_create", "astraea_step_host", "astraea_budget_to_k",
@@ -246,6 +248,14 @@ def astraea_sparse_cross_attn(q, k, v, q_strides, k_strides, v_strides, q_idx, M
     _check(lib().astraea_sparse_cross_attn(_ptr(q), _ptr(k), _ptr(v), *q_strides, *k_strides, *v_strides,
                                            _ptr(q_idx), M, _ptr(out), _ptr(lse_out), B, H, N, N_kv, d, scale, flags,
                                            _ptr(workspace), workspace.numel() if workspace is not None else 0, _stream(stream)))
+
+
+def astraea_window_attn(q, k, v, q_strides, k_strides, v_strides, q_idx, M, out, lse_out, B, H, H_kv, N, d, n_first=0, n_last=0, left=0, right=0,
+                        kv_len=None, scale=0.0, flags=0, workspace=None, stream=None) -> None:
+    """Attention of the listed rows over keys p - left .. p + right around each, the first n_first and the last n_last keys."""
+    _check(lib().astraea_window_attn(_ptr(q), _ptr(k), _ptr(v), *q_strides, *k_strides, *v_strides, _ptr(q_idx), M, _ptr(kv_len),
+                                     _ptr(out), _ptr(lse_out), B, H, H_kv, N, d, n_first, n_last, left, right, scale, flags, _ptr(workspace),
+                                     workspace.numel() if workspace is not None else 0, _stream(stream)))
 
 
 def astraea_scatter_reuse(cache, rows, idx, B, N, M, row_elems, flags=0, workspace=None, stream=None) -> None:

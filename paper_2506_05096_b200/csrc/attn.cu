@@ -45,7 +45,10 @@
 // tcgen05.mma several times slower).  Every mbarrier wait is bounded; on a timeout the CTA raises
 // the error word, the remaining waits return at once, no further copy is sent for, and the CTA runs out; it leaves when
 // the copies and MMAs that were under way have ended.
+#include <limits.h>
+
 #include <mutex>
+#include <type_traits>
 
 #include "common.cuh"
 #include "sm100_ptx.cuh"
@@ -74,7 +77,10 @@ constexpr uint32_t kGaveUpLse = 0xffc0dead;
 // DH: head_dim.  TM: 128-row query tiles per CTA.  Two share every K/V tile in shared memory and run one CTA per SM;
 // one (head_dim 64 / 72 only) lets two CTAs share an SM, which costs ~5 % of throughput per SM but halves the
 // granularity of the schedule: launches of only a few rounds of CTAs are faster with it.
-template <int DH, int TM> struct Cfg {
+// WIN: attention over a window of keys (window_keys.cuh).
+template <int DH, int TM, bool WIN = false> struct Cfg {
+    static constexpr bool kWindow = WIN;
+    static_assert(!WIN || TM == 2, "windows: two query tiles per CTA");
     static_assert(TM == 2 || DH != 128, "head_dim 128 needs the whole SM");
     static constexpr int kDH = DH;
     static constexpr int kTilesM = TM;
@@ -98,7 +104,8 @@ template <int DH, int TM> struct Cfg {
     // (+6 %), and normalises O by the sum of the very bf16 probabilities that went into it; the row sum, and with it
     // the LSE, then carries the bf16 rounding of the probabilities (up to 2^-8 relative when one key dominates a row).
     // head_dim 72 gains nothing from it and 128 has no TMEM columns left: they sum the fp32 exponentials themselves.
-    static constexpr bool kOnes = DH == 64;
+    // (Windows may be short, where that rounding does not average out: they sum the exponentials, too.)
+    static constexpr bool kOnes = DH == 64 && !WIN;
     static constexpr int kSBufs = 2;                              // S buffers per query tile: one per softmax warpgroup
     // Pairs of exponentials that are computed on the FMA pipe instead of the XU: three of eight at head_dim 64, one of four
     // at 72, one of eight in its small CTAs, whose registers do not hold more (62 against 58.5 us for 13106 x 226 x 16; us a
@@ -165,6 +172,9 @@ struct Params {
     int n_ctas, copy_ctas;       // CTAs of the attention, and CTAs behind them that copy the rows (0: the attention's CTAs do)
     float *part_o, *part_lse;    // [part][kTilesM * 128 rows][head_dim] and [part][kTilesM * 128 rows]
 };
+
+#include "window_keys.cuh"
+template <class C> using ParamsOf = std::conditional_t<C::kWindow, WindowParams, Params>;
 
 __device__ __forceinline__ float ex2(float x) {
     float y;
@@ -252,6 +262,15 @@ struct SoftmaxState {
     volatile int *abort_flag;
     int *err_word;
 };
+struct WindowState : SoftmaxState {
+    const KeyList *keys;            // of the CTA (shared memory)
+    int tile0;                      // its first key tile in that list
+    int lo, hi;                     // keys in reach of this thread's row
+    int warp_lo, warp_hi;           // keys in reach of all rows of the warp
+    int n_first, last0;
+    bool seen;                      // some key of the CTA's tiles is visible to the row
+};
+template <class C> using StateOf = std::conditional_t<C::kWindow, WindowState, SoftmaxState>;
 
 // the 64 columns of one S buffer into registers (asynchronous: wait_s_regs before using them)
 template <int NS>
@@ -331,7 +350,7 @@ enum { kSpeculate = 0, kMaxOnly = 1, kExact = 2 };
 // One key tile of the softmax.  j: key tile; g: running count of S-buffer uses of this query tile (buffer
 // g % kSBufs, barrier phase (g / kSBufs) & 1), which keeps counting across the passes.
 template <class C, int MODE>
-__device__ __forceinline__ void softmax_step(SoftmaxState &st, int j, int g)
+__device__ __forceinline__ void softmax_step(StateOf<C> &st, int j, int g)
 {
     constexpr int kSBufs = C::kSBufs, NS = C::kBlockN;
     const int buf = g % kSBufs;
@@ -344,7 +363,15 @@ __device__ __forceinline__ void softmax_step(SoftmaxState &st, int j, int g)
     tc_fence_after();
     load_s<NS>(t_s, cur);
     wait_s_regs<NS>(cur);
-    mask_tail<NS>(cur, st.N - j * NS);
+    uint64_t visible = ~0ull;                          // keys of the tile that this row sees
+    bool some_hidden = false;                          // for the warp
+    if constexpr (C::kWindow) {
+        const int k0 = st.keys->key(st.tile0 + j), end = st.keys->end(st.tile0 + j);
+        some_hidden = !sees_all(k0, end, st.warp_lo, st.warp_hi, st.n_first, st.last0);
+        if (some_hidden) visible = visible_bits(k0, end, st.lo, st.hi, st.n_first, st.last0);
+        st.seen |= visible != 0;
+        if (MODE == kMaxOnly && some_hidden) hide<NS>(cur, visible, -INFINITY);
+    } else mask_tail<NS>(cur, st.N - j * NS);
     if constexpr (MODE == kMaxOnly) {
         st.m_ref = fmaxf(st.m_ref, row_max<NS>(cur));
         tc_fence_before();
@@ -369,6 +396,7 @@ __device__ __forceinline__ void softmax_step(SoftmaxState &st, int j, int g)
             cur[i] = ex2(cur[i]); cur[i + 1] = ex2(cur[i + 1]);
         }
     }
+    if constexpr (C::kWindow) { if (some_hidden) hide<NS>(cur, visible, 0.f); }
     float tile_sum = 0.f;
     if constexpr (!C::kOnes) {
         unsigned long long a[4] = {0ull, 0ull, 0ull, 0ull};
@@ -404,9 +432,10 @@ __device__ __forceinline__ void pass_sync() {
 // ---------------------------------------------------------------- softmax warpgroup
 // tile: its query tile; par: which key tiles it takes (j = par, par + kSplit, ...)
 template <class C>
-__device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, int tile, int par, uint8_t *sQ_gen, uint32_t tmem,
+__device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &bar, int tile, int par, uint8_t *sQ_gen, uint32_t tmem,
                                              int m_base, int h, int b, int n_tiles, int key0, int part, bool last_unit,
-                                             volatile int *abort_flag, volatile int *redo_flag, float2 *xchg)
+                                             volatile int *abort_flag, volatile int *redo_flag, float2 *xchg,
+                                             const KeyList *keys = nullptr, int tile0 = 0, volatile int *odd_flag = nullptr)
 {
     const int wtid = threadIdx.x & 127;
     const int warp = __shfl_sync(0xffffffffu, wtid >> 5, 0);       // warp-uniform
@@ -423,6 +452,9 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
         const int r = v / kUnits, c = v - r * kUnits;
         const int m = m_base + r;
         gtok[it] = -1;
+        if constexpr (C::kWindow) {                      // row m of the unit: query m / group of the list, head m % group of the key head
+            if (m < p.M * p.group && c * 8 < C::kDH) gtok[it] = p.q_compact ? m / p.group : p.token(b, m / p.group);
+        } else
         if (m < p.M && c * 8 < C::kDH)                   // the upper half of the tail chunk stays zero
             gtok[it] = p.q_idx ? __ldcg(p.q_idx + (size_t)b * p.M + m) : m;
     }
@@ -433,7 +465,9 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
         const int c = v % kUnits;
         gval[it] = make_uint4(0, 0, 0, 0);
         if ((unsigned)gtok[it] < (unsigned)p.N_tok) {
-            const __nv_bfloat16 *src = p.q + (size_t)b * p.q_sb + (size_t)gtok[it] * p.q_sn + (size_t)h * p.q_sh + c * 8;
+            int head = h;
+            if constexpr (C::kWindow) head = h * p.group + (m_base + v / kUnits) % p.group;
+            const __nv_bfloat16 *src = p.q + (size_t)b * p.q_sb + (size_t)gtok[it] * p.q_sn + (size_t)head * p.q_sh + c * 8;
             gval[it] = __ldcg(reinterpret_cast<const uint4 *>(src));
         }
     }
@@ -450,7 +484,7 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
     mbar_arrive(bar.q + 8 * tile);
 
     const uint32_t t_row = tmem + ((uint32_t)(warp * 32) << 16);
-    SoftmaxState st;
+    StateOf<C> st;
     st.sl2 = p.scale_log2;
     st.l_sum = 0.f;
     st.t_s0 = t_row + tile * C::kSBufs * C::kBlockN;
@@ -460,7 +494,12 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
     st.abort_flag = abort_flag; st.err_word = p.err_word;
     st.ref_x = &xchg[wtid].x; st.ref_bar = 3 + tile; st.redo_flag = redo_flag;
 
-    const int m = m_base + wtid;
+    int m = m_base + wtid;
+    if constexpr (C::kWindow) {
+        const int g = m % p.group;
+        m /= p.group;
+        h = h * p.group + g;                                     // this row's head
+    }
     int tok = -1;
     if (m < p.M) {
         tok = p.q_idx ? __ldcg(p.q_idx + (size_t)b * p.M + m) : m;
@@ -471,16 +510,34 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
         if (bad) { if (par == 0 && p.err_word) atomicExch(p.err_word, kErrBadIndex); tok = -1; }
     }
 
+    if constexpr (C::kWindow) {
+        st.keys = keys; st.tile0 = tile0;
+        st.n_first = p.n_first; st.last0 = p.last0;
+        st.lo = tok - p.left; st.hi = tok + p.right;
+        st.warp_lo = __reduce_max_sync(0xffffffffu, tok >= 0 ? st.lo : INT_MIN);
+        st.warp_hi = __reduce_min_sync(0xffffffffu, tok >= 0 ? st.hi : INT_MAX);
+        st.seen = false;
+    }
     st.m_ref = -INFINITY;
     st.shift = kRefShift;
-    if (par == 1) {
+    const bool no_keys = C::kWindow && n_tiles == 0;
+    if (par == 1 && !no_keys) {
         // the even-tile warpgroup takes the exact row maxima of key tile 0 and hands them over
         if (tile == 0) asm volatile("bar.sync 3, 256;" ::: "memory");
         else asm volatile("bar.sync 4, 256;" ::: "memory");
         st.m_ref = *st.ref_x;
     }
     for (int j = par; j < n_tiles; j += kSplit) softmax_step<C, kSpeculate>(st, j, j);
-    wait_bar(st.bar_done, 0, abort_flag, p.err_word);            // every P V of this query tile has landed
+    if (!no_keys) wait_bar(st.bar_done, 0, abort_flag, p.err_word);            // every P V of this query tile has landed
+    if constexpr (C::kWindow) {
+        // The reference is the largest logit of the first key tile, seen or not: where all that the row sees lies far below it, small
+        // terms are lost (a sum of 2^-80 still has 26 bits between its largest term and the smallest normal number)
+        xchg[wtid + par * kBlockM] = make_float2(st.seen ? 1.f : 0.f, st.l_sum);
+        pair_sync(tile);
+        const float2 other = xchg[wtid + (par ^ 1) * kBlockM];
+        st.seen |= other.x != 0.f;
+        if (__any_sync(0xffffffffu, tok >= 0 && st.seen && !(st.l_sum + other.y >= kLeastSum))) *redo_flag = 1;
+    }
     if constexpr (C::kOnes) {
         // the row sum came out of the tensor core with O; one that passed the limit (or is inf / NaN) means that
         // the reference was too low somewhere along the row
@@ -500,6 +557,7 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
         if (tile == 0) asm volatile("bar.sync 1, 256;" ::: "memory");
         else asm volatile("bar.sync 2, 256;" ::: "memory");
         st.m_ref = fmaxf(xchg[wtid].x, xchg[wtid + kBlockM].x);
+        if (C::kWindow && st.m_ref == -INFINITY) st.m_ref = 0.f;  // nothing that counts is seen: all terms are 0 against any reference
         st.shift = 0.f;
         st.l_sum = 0.f;
         for (int j = par; j < n_tiles; j += kSplit) softmax_step<C, kExact>(st, j, 2 * n_tiles + j);
@@ -528,41 +586,62 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
     }
     constexpr int ncol = C::kMain / 2;                           // O columns this thread writes
     const int col0 = par * ncol;
-    const float inv_l = 1.0f / l_sum;
+    float inv_l = 1.0f / l_sum;
+    if constexpr (C::kWindow) {                                  // a row that sees nothing is zero, its LSE -inf (log 0)
+        if (!st.seen) { l_sum = 0.f; st.m_ref = 0.f; st.shift = 0.f; }
+        if (l_sum == 0.f) inv_l = 0.f;
+    }
+    // 32 columns (or the 8 of the tail) of O; a CTA without keys has none
+    auto load_o = [&](uint32_t col, auto &o) {
+        if constexpr (sizeof(o) == 128) tmem_ld32(st.t_o + col, o); else tmem_ld8(st.t_o + col, o);
+        tc_wait_ld();
+        if constexpr (C::kWindow) {
+            if (no_keys)
+#pragma unroll
+                for (uint32_t &w : o) w = 0u;
+        }
+    };
+    // window: values that were cleared (see clear_odd) go back into the rows that see them
+    auto put_back = [&](auto *row) {
+        if constexpr (C::kWindow) {
+            const bool odd = pair_any(tile, *odd_flag != 0);     // (the row's two halves have been written; one answer for both warpgroups)
+            if (odd && par == 0 && row) spread_odd_values<std::remove_pointer_t<decltype(row)>, C::kDH>(p, *keys, tile0, n_tiles, b, h / p.group, tok, row);
+        }
+    };
     if (part >= 0) {
         // a share of the keys only: the normalised row and its LSE go to the workspace in fp32 (every row of the tile,
         // listed or not; the merge knows which ones count).  A CTA that gave up marks its rows.
         const size_t prow = (size_t)part * (C::kTilesM * kBlockM) + tile * kBlockM + wtid;
         float *po = p.part_o + prow * C::kDH;
-        if (par == 0)
+        const bool write = !C::kWindow || m < p.M;               // (window: a unit may have a handful of rows)
+        if (par == 0 && write)
             p.part_lse[prow] = *abort_flag ? __uint_as_float(kGaveUpLse) : st.m_ref * p.scale + st.shift * 0.6931471805599453f + logf(l_sum);
 #pragma unroll
         for (int cc = 0; cc < ncol; cc += 32) {
             const int c = col0 + cc;
             uint32_t o[32];
-            tmem_ld32(st.t_o + c, o);
-            tc_wait_ld();
+            load_o(c, o);
 #pragma unroll
             for (int v = 0; v < 8; ++v)
-                *reinterpret_cast<float4 *>(po + c + v * 4) = make_float4(__uint_as_float(o[4 * v]) * inv_l, __uint_as_float(o[4 * v + 1]) * inv_l,
+                if (write) *reinterpret_cast<float4 *>(po + c + v * 4) = make_float4(__uint_as_float(o[4 * v]) * inv_l, __uint_as_float(o[4 * v + 1]) * inv_l,
                                                                            __uint_as_float(o[4 * v + 2]) * inv_l, __uint_as_float(o[4 * v + 3]) * inv_l);
         }
         if (C::kTail && par == kSplit - 1) {
             uint32_t o[8];
-            tmem_ld8(st.t_o + C::kMain, o);
-            tc_wait_ld();
+            load_o(C::kMain, o);
 #pragma unroll
             for (int v = 0; v < 2; ++v)
-                *reinterpret_cast<float4 *>(po + C::kMain + v * 4) = make_float4(__uint_as_float(o[4 * v]) * inv_l, __uint_as_float(o[4 * v + 1]) * inv_l,
+                if (write) *reinterpret_cast<float4 *>(po + C::kMain + v * 4) = make_float4(__uint_as_float(o[4 * v]) * inv_l, __uint_as_float(o[4 * v + 1]) * inv_l,
                                                                                   __uint_as_float(o[4 * v + 2]) * inv_l, __uint_as_float(o[4 * v + 3]) * inv_l);
         }
+        put_back(tok >= 0 ? po : nullptr);
         return;
     }
     __nv_bfloat16 *dst = nullptr;
     long long orow_ok = -1;                                      // this thread's output row, or -1: nothing is written
     if (tok >= 0 && !*abort_flag) {
         const size_t orow = p.compact ? ((size_t)b * p.M + m) : ((size_t)b * p.N_tok + tok);
-        orow_ok = (long long)orow;
+        orow_ok = C::kWindow ? (long long)(orow * p.H + h) : (long long)orow;      // (window: the rows of a tile are of several heads)
         dst = p.out + (orow * p.H + h) * C::kDH;
         if (p.lse_out && par == 0) {
             const size_t li = p.compact ? (((size_t)b * p.H + h) * p.M + m) : (((size_t)b * p.H + h) * p.N_tok + tok);
@@ -582,8 +661,7 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
     for (int cc = 0; cc < ncol; cc += 32) {
         const int c = col0 + cc;
         uint32_t o[32];
-        tmem_ld32(st.t_o + c, o);
-        tc_wait_ld();
+        load_o(c, o);
         if constexpr (!kStagedStores) {
             if (dst) {
 #pragma unroll
@@ -614,15 +692,15 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
                 const int r = (lane >> 2) + 8 * jj;
                 const long long orow_r = __shfl_sync(0xffffffffu, orow_ok, r);
                 const uint4 t = *reinterpret_cast<const uint4 *>(stage + r * 64 + ((q4 ^ ((r >> 1) & 3)) << 4));
-                if (orow_r >= 0) *reinterpret_cast<uint4 *>(p.out + ((size_t)orow_r * p.H + h) * C::kDH + c + q4 * 8) = t;
+                const size_t to = C::kWindow ? (size_t)orow_r : (size_t)orow_r * p.H + h;
+                if (orow_r >= 0) *reinterpret_cast<uint4 *>(p.out + to * C::kDH + c + q4 * 8) = t;
             }
             __syncwarp();
         }
     }
     if (C::kTail && par == kSplit - 1) {
         uint32_t o[8], w[4];
-        tmem_ld8(st.t_o + C::kMain, o);
-        tc_wait_ld();
+        load_o(C::kMain, o);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             __nv_bfloat162 v2 = __floats2bfloat162_rn(__uint_as_float(o[2 * i]) * inv_l, __uint_as_float(o[2 * i + 1]) * inv_l);
@@ -630,6 +708,7 @@ __device__ __forceinline__ void softmax_role(const Params &p, const Bars &bar, i
         }
         if (dst) *reinterpret_cast<uint4 *>(dst + C::kMain) = make_uint4(w[0], w[1], w[2], w[3]);
     }
+    put_back(dst);
 }
 
 #include "copy_rows.cuh"
@@ -661,7 +740,7 @@ __device__ __forceinline__ void copy_cta(const Params &p, int cta)
 template <class C>
 __global__ void __launch_bounds__(C::kThreads, C::kCtasPerSM)
 sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
-                   const __grid_constant__ CUtensorMap tmap_k_tail, const __grid_constant__ CUtensorMap tmap_v_tail, const Params p)
+                   const __grid_constant__ CUtensorMap tmap_k_tail, const __grid_constant__ CUtensorMap tmap_v_tail, const __grid_constant__ ParamsOf<C> p)
 {
     constexpr int kTilesM = C::kTilesM;
     constexpr uint32_t kTmemCols = C::kTmemCols;
@@ -672,6 +751,9 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     __shared__ int k_stop, v_stop;                                 // the K and V tiles that were sent for before the CTA gave up
     __shared__ volatile int redo_flag;
     __shared__ float2 xchg[C::kTilesM][2 * kBlockM];
+    // windows: the key tiles of the unit; whether a value was cleared (see window_keys.cuh)
+    __shared__ std::conditional_t<C::kWindow, KeyList, char> key_list;
+    __shared__ std::conditional_t<C::kWindow, int, char> odd_values;
 
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t *smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
@@ -688,7 +770,9 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     bar.vf = bar.ke + 8 * C::kStagesK;
     bar.ve = bar.vf + 8 * C::kStagesV;
     const uint32_t bar_copy = bar.ve + 8 * C::kStagesV, bar_end = bar_copy + 8 * C::kCopyStages;
-    static_assert(160 + 16 * (C::kStagesK + C::kStagesV) + 8 * (C::kCopyStages + 2) <= C::kBarBytes, "barrier area too small");
+    const uint32_t bar_vr = bar_end + 16;                          // windows: the values of a stage have been looked at
+    static_assert(160 + 16 * (C::kStagesK + C::kStagesV) + 8 * (C::kCopyStages + 2) + (C::kWindow ? 8 * C::kStagesV : 0) <= C::kBarBytes,
+                  "barrier area too small");
 
     if ((int)blockIdx.x >= p.n_ctas) {
         copy_cta(p, (int)blockIdx.x - p.n_ctas);
@@ -707,11 +791,24 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     }
     int m0 = (unit % p.tiles_x) * (kTilesM * kBlockM), h = p.h0 + (unit / p.tiles_x) % p.heads, b = unit / (p.tiles_x * p.heads);
     const int n_tiles_all = (p.N + kBlockN - 1) / kBlockN;
-    const int tile0 = n_tiles_all * kpart / ksplit;                // first key tile of this CTA (split <= 8: no overflow)
-    const int n_tiles = n_tiles_all * (kpart + 1) / ksplit - tile0;
+    int tile0 = n_tiles_all * kpart / ksplit;                      // first key tile of this CTA (split <= 16, windows: N <= 2^30: no overflow)
+    int n_tiles = n_tiles_all * (kpart + 1) / ksplit - tile0;
     const int key0 = tile0 * kBlockN;
+    // first key of the CTA's key tile j
+    auto key_of = [&](int j) -> int {
+        if constexpr (C::kWindow) return key_list.key(tile0 + j); else return key0 + j * kBlockN;
+    };
     // the last CTA of a head may have rows in its first query tile only: the second tile's warps and MMAs are skipped
-    const int q_tiles = (kTilesM > 1 && m0 + kBlockM < p.M) ? kTilesM : 1;
+    int n_rows = p.M;
+    if constexpr (C::kWindow) n_rows = p.M * p.group;
+    const int q_tiles = (kTilesM > 1 && m0 + kBlockM < n_rows) ? kTilesM : 1;
+    // windows: this CTA's share of the unit's key tiles
+    auto take_share = [&] {
+        if constexpr (C::kWindow) {
+            tile0 = key_list.n * kpart / ksplit;
+            n_tiles = key_list.n * (kpart + 1) / ksplit - tile0;
+        }
+    };
 
     if constexpr (C::kOnes) {
         // row r: 128 bytes; under the 128-byte swizzle the 16-byte unit that holds column 0 is unit r & 7
@@ -736,6 +833,10 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         redo_flag = 0;
         init_query_bars();
         for (int u = 0; u < C::kCopyStages + 2; ++u) mbar_init(bar_copy + 8 * u, 1);       // (and bar_end)
+        if constexpr (C::kWindow) {
+            odd_values = 0;
+            for (int u = 0; u < C::kStagesV; ++u) mbar_init(bar_vr + 8 * u, 1);
+        }
         fence_barrier_init();
     }
     constexpr int kProducerWarp = C::kSoftmaxWarps, kIssuerWarp = C::kSoftmaxWarps + 1;
@@ -749,21 +850,44 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         fence_barrier_init();
     };
     auto send_first_tiles = [&] {
+        if (C::kWindow && n_tiles == 0) return;
         for (int j = 0; j < kAhead && j < n_tiles; ++j) {
             mbar_arrive_expect_tx(bar.kf + 8 * j, C::kLoadBytes);
 #pragma unroll
             for (int ch = 0; ch < C::kChunks; ++ch)
-                tma_load_4d(sK + j * C::kTileBytes + ch * C::kChunkBytes, &tmap_k, bar.kf + 8 * j, ch * 64, key0 + j * kBlockN, h, b);
+                tma_load_4d(sK + j * C::kTileBytes + ch * C::kChunkBytes, &tmap_k, bar.kf + 8 * j, ch * 64, key_of(j), h, b);
             if (C::kTail)
-                tma_load_4d(sK + j * C::kTileBytes + C::kChunks * C::kChunkBytes, &tmap_k_tail, bar.kf + 8 * j, C::kMain, key0 + j * kBlockN, h, b);
+                tma_load_4d(sK + j * C::kTileBytes + C::kChunks * C::kChunkBytes, &tmap_k_tail, bar.kf + 8 * j, C::kMain, key_of(j), h, b);
         }
         mbar_arrive_expect_tx(bar.vf, C::kLoadBytes);
 #pragma unroll
         for (int ch = 0; ch < C::kChunks; ++ch)
-            tma_load_4d(sV + ch * C::kChunkBytes, &tmap_v, bar.vf, ch * 64, key0, h, b);
+            tma_load_4d(sV + ch * C::kChunkBytes, &tmap_v, bar.vf, ch * 64, key_of(0), h, b);
         if (C::kTail)
-            tma_load_4d(sV + C::kChunks * C::kChunkBytes, &tmap_v_tail, bar.vf, C::kMain, key0, h, b);
+            tma_load_4d(sV + C::kChunks * C::kChunkBytes, &tmap_v_tail, bar.vf, C::kMain, key_of(0), h, b);
     };
+    if constexpr (C::kWindow) {
+        // The producer warp needs the positions of the unit's rows before it can send for anything: it reads the list and says which key
+        // tiles there are.  Entries that are not written (see softmax_role) do not count.
+        if (warp == kProducerWarp) {
+            grid_dependency_wait();
+            const int m_first = m0 / p.group, m_end = min(p.M, (m0 + kTilesM * kBlockM - 1) / p.group + 1);
+            int first = INT_MAX, last = -1;
+            constexpr int kEntries = kTilesM * kBlockM / 32 + 1;
+#pragma unroll
+            for (int i = 0; i < kEntries; ++i) {
+                const int m = m_first + i * 32 + (tid & 31);
+                const int tok = m < m_end ? p.token(b, m) : -1;
+                if ((unsigned)tok < (unsigned)p.N_tok) { first = min(first, tok); last = max(last, tok); }
+            }
+            first = __reduce_min_sync(0xffffffffu, first);
+            last = __reduce_max_sync(0xffffffffu, last);
+            const KeyList k = list_keys(p, b, first, last);
+            if ((tid & 31) == 0) key_list = k;
+            __syncwarp();
+            take_share();
+        }
+    }
     if (warp == kProducerWarp) {
         if (elect_one()) {
             prefetch_tensormap(&tmap_k); prefetch_tensormap(&tmap_v);
@@ -783,6 +907,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = tmem_slot;
     grid_dependency_wait();
+    take_share();
 
     // Persistent CTAs: on to the next unit, if there is one (called by every warp, from its role).  Between the two CTA-wide
     // barriers nothing of the last unit is in flight (the producer has waited for its copies and for the issuers' last commits, the
@@ -825,10 +950,14 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         const int wg = warp >> 2;
         const int tile = wg / kSplit, par = wg % kSplit;
         do {
-            if (tile < q_tiles)
+            if (tile < q_tiles) {
+                if constexpr (C::kWindow)
+                    softmax_role<C>(p, bar, tile, par, smem_gen + tile * C::kQTileBytes, tmem, m0 + tile * kBlockM, h, b, n_tiles, 0, part,
+                                     true, &abort_flag, &redo_flag, xchg[tile], &key_list, tile0, &odd_values);
+                else
                 softmax_role<C>(p, bar, tile, par, smem_gen + tile * C::kQTileBytes, tmem, m0 + tile * kBlockM, h, b, n_tiles, key0, part,
                                  !C::kPersistent || unit + p.n_ctas >= n_units, &abort_flag, &redo_flag, xchg[tile]);
-            else pass_sync<C>();
+            } else pass_sync<C>();
         } while (next_unit());
     } else if (warp == kProducerWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsOther));
@@ -846,9 +975,9 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 mbar_arrive_expect_tx(bar.kf + 8 * st, C::kLoadBytes);
 #pragma unroll
                 for (int ch = 0; ch < C::kChunks; ++ch)
-                    tma_load_4d(sK + st * C::kTileBytes + ch * C::kChunkBytes, &tmap_k, bar.kf + 8 * st, ch * 64, key0 + j * kBlockN, h, b);
+                    tma_load_4d(sK + st * C::kTileBytes + ch * C::kChunkBytes, &tmap_k, bar.kf + 8 * st, ch * 64, key_of(j), h, b);
                 if (C::kTail)
-                    tma_load_4d(sK + st * C::kTileBytes + C::kChunks * C::kChunkBytes, &tmap_k_tail, bar.kf + 8 * st, C::kMain, key0 + j * kBlockN, h, b);
+                    tma_load_4d(sK + st * C::kTileBytes + C::kChunks * C::kChunkBytes, &tmap_k_tail, bar.kf + 8 * st, C::kMain, key_of(j), h, b);
             }
             __syncwarp();
         };
@@ -859,9 +988,9 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 mbar_arrive_expect_tx(bar.vf + 8 * st, C::kLoadBytes);
 #pragma unroll
                 for (int ch = 0; ch < C::kChunks; ++ch)
-                    tma_load_4d(sV + st * C::kTileBytes + ch * C::kChunkBytes, &tmap_v, bar.vf + 8 * st, ch * 64, key0 + j * kBlockN, h, b);
+                    tma_load_4d(sV + st * C::kTileBytes + ch * C::kChunkBytes, &tmap_v, bar.vf + 8 * st, ch * 64, key_of(j), h, b);
                 if (C::kTail)
-                    tma_load_4d(sV + st * C::kTileBytes + C::kChunks * C::kChunkBytes, &tmap_v_tail, bar.vf + 8 * st, C::kMain, key0 + j * kBlockN, h, b);
+                    tma_load_4d(sV + st * C::kTileBytes + C::kChunks * C::kChunkBytes, &tmap_v_tail, bar.vf + 8 * st, C::kMain, key_of(j), h, b);
             }
             __syncwarp();
         };
@@ -947,7 +1076,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 const bool more = j + kAhead < n_tiles;
                 const int sk = (gk0 + j + kAhead) % C::kStagesK;
                 if (more) wait_bar(bar.kf + 8 * sk, ((gk0 + j + kAhead) / C::kStagesK) & 1, &abort_flag, p.err_word);
-                if (with_v) wait_bar(bar.vf + 8 * sv, ((gv0 + j) / C::kStagesV) & 1, &abort_flag, p.err_word);
+                if (with_v) wait_bar((C::kWindow ? bar_vr : bar.vf) + 8 * sv, ((gv0 + j) / C::kStagesV) & 1, &abort_flag, p.err_word);
                 // P of key tile j is in TMEM (max-only pass: S of key tile j has been read)
                 wait_bar(bar.p + 32 * t + 8 * u, ((gs0 + j) / kSBufs) & 1, &abort_flag, p.err_word);
                 tc_fence_after();
@@ -986,6 +1115,35 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 issue_pass(kExact);
             }
         } while (next_unit());
+    } else if constexpr (C::kWindow) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsOther));
+        // ------------------------------------------------ looks at the values of a stage before the MMAs (see clear_odd)
+        const int lane = tid & 31;
+        auto look_pass = [&](int gv0) {
+            for (int j = 0; j < n_tiles; ++j) {
+                const int sv = (gv0 + j) % C::kStagesV;
+                wait_bar(bar.vf + 8 * sv, ((gv0 + j) / C::kStagesV) & 1, &abort_flag, p.err_word);
+                const int k0 = key_of(j), end = key_list.end(tile0 + j);
+                if (!sees_all(k0, end, key_list.all_lo, key_list.all_hi, p.n_first, p.last0)) {
+                    uint4 *v = reinterpret_cast<uint4 *>(smem_gen + (sV - smem_base) + sv * C::kTileBytes);
+                    bool odd = false;
+                    // rows of 128 bytes in each chunk, of 32 in the tail (the swizzle keeps a row's bytes in its row)
+#pragma unroll 4
+                    for (int i = lane; i < C::kLoadBytes / 16; i += 32) {
+                        const int row = i < C::kChunks * C::kChunkBytes / 16 ? i / 8 % kBlockN : (i - C::kChunks * C::kChunkBytes / 16) / 2;
+                        const uint4 is = v[i], to = k0 + row < end ? clear_odd(is, odd) : make_uint4(0, 0, 0, 0);
+                        if (is.x != to.x || is.y != to.y || is.z != to.z || is.w != to.w) v[i] = to;
+                    }
+                    if (odd) *static_cast<volatile int *>(&odd_values) = 1;
+                    fence_proxy_async_smem();
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_vr + 8 * sv);
+            }
+        };
+        look_pass(0);
+        pass_sync<C>();
+        if (redo_flag) look_pass(n_tiles);
     } else {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsOther));
         // The pass does not wait for the rows that it copies (a CTA of a few key tiles is done before them): it is counted ahead.
@@ -1100,7 +1258,6 @@ int32_t make_kv_map(CUtensorMap *map, const void *base, int B, int H, int N, int
 struct SplitPlan { int units = 0, split = 1; };
 
 constexpr int kMaxSplit = 8;                 // shares per unit
-constexpr int kMaxSplitParts = 2 * 148;      // shares per launch (what the workspace holds)
 constexpr int kMinSplitKeyTiles = 16;        // key tiles per share at least
 
 template <int DH, int TM>
@@ -1202,7 +1359,7 @@ int32_t launch_dh(const AttnArgs &a, cudaStream_t stream, SplitPlan plan = Split
 
 // 256 bytes for the error word; behind them room for the key shares of a split last round of CTAs (fp32 rows and
 // LSEs), an upper bound over every M' <= M of the same problem
-static size_t split_bytes(long long parts, int d) { return (size_t)parts * (2 * kBlockM) * ((size_t)d * 4 + 4) + 256; }
+static_assert(2 * kBlockM == 256, "split_bytes counts the rows of a unit");
 static int max_split_of(int N) { const int s = ((N + 63) / 64) / kMinSplitKeyTiles; return s > kMaxSplit ? kMaxSplit : s; }
 
 size_t attn_workspace_bytes(int B, int H, int N, int M, int d)
@@ -1331,7 +1488,7 @@ int32_t launch_wait_selftest(int *err_word, uint64_t limit_ns, int *gave_up, cud
 namespace {
 struct Schedule { bool small = false; SplitPlan plan; };
 
-double finish_time(long long units, int pairs, bool light_last, int n_sm, int tail_units, int split)
+double finish_time(long long units, int pairs, bool light_last, int n_sm, int tail_units, int split, double share_cost = 0.03)
 {
     // greedy dispatch in launch order: every CTA goes to the SM that is free first (a binary min-heap of busy times)
     double heap[kMaxSMs] = {};
@@ -1354,7 +1511,7 @@ double finish_time(long long units, int pairs, bool light_last, int n_sm, int ta
     for (long long c = 0; c < units; ++c) {
         const double cost = (light_last && c % pairs == pairs - 1) ? 0.68 : 1.0;
         if (c < units - tail_units) put(cost);
-        else for (int i = 0; i < split; ++i) put(cost / split + 0.03);
+        else for (int i = 0; i < split; ++i) put(cost / split + share_cost);
     }
     return finish;
 }
@@ -1424,6 +1581,168 @@ int32_t launch_sparse_attn(const AttnArgs &a, cudaStream_t stream)
     }
     case 128: return launch_dh<128, 2>(a, stream, choose_schedule(a, 0.0).plan);
     default: return fail(ASTRAEA_ERR_UNSUPPORTED, "head_dim %d is not supported", a.d);
+    }
+}
+
+// ---------------------------------------------------------------- a window of keys (astraea_window_attn)
+namespace {
+// Combines the key shares of split units, as merge_parts_kernel does.  Shares come in fours, so that a thread holds the rows of four; a
+// share whose keys a row does not see has an LSE of -inf and no weight, and a row that sees no key at all is zero.
+template <int DH, int ROWS>
+__global__ void __launch_bounds__(ROWS) merge_window_kernel(const __grid_constant__ WindowParams p)
+{
+    constexpr int kChunksRow = DH / 8;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int unit = p.n_full + blockIdx.y;
+    const int m0 = (unit % p.tiles_x) * ROWS, kv = (unit / p.tiles_x) % p.heads, b = unit / (p.tiles_x * p.heads);
+    const int idx = blockIdx.x * ROWS + threadIdx.x;
+    const int r = idx / kChunksRow, c = idx - r * kChunksRow;
+    if (m0 + r >= p.M * p.group) return;
+    const int m = (m0 + r) / p.group, h = kv * p.group + (m0 + r) % p.group;
+    const int tok = p.token(b, m), before = (p.q_idx && m > 0) ? p.token(b, m - 1) : -1;
+    const size_t part0 = (size_t)blockIdx.y * p.split;
+    float lse[kMaxWindowSplit], mx = -INFINITY;
+    bool gave_up = false;
+#pragma unroll
+    for (int i = 0; i < kMaxWindowSplit; ++i) lse[i] = i < p.split ? __ldcg(p.part_lse + (part0 + i) * ROWS + r) : -INFINITY;
+#pragma unroll
+    for (int i = 0; i < kMaxWindowSplit; ++i) {
+        gave_up |= __float_as_uint(lse[i]) == kGaveUpLse;
+        mx = fmaxf(mx, lse[i]);
+    }
+    if ((unsigned)tok >= (unsigned)p.N_tok || before >= tok || gave_up) return;       // reported by the attention kernel
+    const float ref = mx == -INFINITY ? 0.f : mx;
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, wsum = 0.f;
+#pragma unroll
+    for (int i0 = 0; i0 < kMaxWindowSplit; i0 += 4) {
+        if (i0 >= p.split) break;
+        float4 x[4], y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i0 + i >= p.split) break;
+            const float4 *src = reinterpret_cast<const float4 *>(p.part_o + ((part0 + i0 + i) * ROWS + r) * DH + c * 8);
+            x[i] = __ldcg(src); y[i] = __ldcg(src + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i0 + i >= p.split) break;
+            const float w = __expf(lse[i0 + i] - ref);
+            wsum += w;
+            acc[0] += w * x[i].x; acc[1] += w * x[i].y; acc[2] += w * x[i].z; acc[3] += w * x[i].w;
+            acc[4] += w * y[i].x; acc[5] += w * y[i].y; acc[6] += w * y[i].z; acc[7] += w * y[i].w;
+        }
+    }
+    const float inv = wsum == 0.f ? 0.f : 1.0f / wsum;
+    uint32_t w4[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        __nv_bfloat162 v2 = __floats2bfloat162_rn(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+        w4[i] = *reinterpret_cast<uint32_t *>(&v2);
+    }
+    const size_t orow = p.compact ? ((size_t)b * p.M + m) : ((size_t)b * p.N_tok + tok);
+    *reinterpret_cast<uint4 *>(p.out + (orow * p.H + h) * DH + c * 8) = make_uint4(w4[0], w4[1], w4[2], w4[3]);
+    if (p.lse_out && c == 0) {
+        const size_t li = p.compact ? (((size_t)b * p.H + h) * p.M + m) : (((size_t)b * p.H + h) * p.N_tok + tok);
+        p.lse_out[li] = ref + logf(wsum);
+    }
+}
+
+// Key tiles that a unit has, as far as the host can tell: 256 rows of an evenly spread list and what is in reach of them.
+long long window_tiles(const WindowArgs &a)
+{
+    const long long rows = a.a.M < 256 / a.group + 1 ? a.a.M : 256 / a.group + 1;
+    const long long span = a.a.M > 1 ? rows * a.a.N_tok / a.a.M : 1, keys = span + a.left + a.right + a.n_first + a.n_last;
+    return ((keys < a.a.N ? keys : a.a.N) + kKeyTile - 1) / kKeyTile;
+}
+
+// The last, partial round of CTAs shares its units' key tiles where that finishes earlier.  A share costs about what four key tiles do on
+// top of its own (positions, query rows, the pipeline, its fp32 rows and their part in the merge).
+SplitPlan window_plan(const WindowArgs &a)
+{
+    SplitPlan plan;
+    const long long rows = (long long)a.a.M * a.group, hb = (long long)a.a.H / a.group * a.a.B;
+    const int pairs = (int)((rows + 2 * kBlockM - 1) / (2 * kBlockM)), n_sm = sm_count();
+    const long long units = hb * pairs;
+    const bool light_last = rows - (long long)(pairs - 1) * 2 * kBlockM <= kBlockM;
+    if (!a.a.split_ws || units > 16 * n_sm) return plan;
+    const long long tiles = window_tiles(a);
+    const int tail = (int)(units % n_sm);
+    if (tail == 0) return plan;
+    const double whole = finish_time(units, pairs, light_last, n_sm, 0, 1);
+    double best = whole;
+    for (int s = 2; s <= kMaxWindowSplit && s * 2 <= tiles; ++s) {
+        if ((long long)tail * s > kMaxSplitParts || split_bytes((long long)tail * s, a.a.d) > a.a.split_ws_bytes) break;
+        const double t = finish_time(units, pairs, light_last, n_sm, tail, s, 4.0 / (double)tiles);
+        if (t < 0.97 * whole && t < best) { best = t; plan.units = tail; plan.split = s; }
+    }
+    return plan;
+}
+
+template <int DH>
+int32_t launch_window_dh(const WindowArgs &w, cudaStream_t stream)
+{
+    using C = Cfg<DH, 2, true>;
+    const AttnArgs &a = w.a;
+    const int kv_heads = a.H / w.group;
+    CUtensorMap mk, mv, mkt, mvt;
+    int32_t rc = make_kv_map(&mk, a.k, a.B, kv_heads, a.N, a.d, a.k_sb, a.k_sh, a.k_sn, false, C::kBlockN);
+    if (rc == ASTRAEA_OK) rc = make_kv_map(&mv, a.v, a.B, kv_heads, a.N, a.d, a.v_sb, a.v_sh, a.v_sn, false, C::kBlockN);
+    mkt = mk; mvt = mv;
+    if (C::kTail && rc == ASTRAEA_OK) rc = make_kv_map(&mkt, a.k, a.B, kv_heads, a.N, a.d, a.k_sb, a.k_sh, a.k_sn, true, C::kBlockN);
+    if (C::kTail && rc == ASTRAEA_OK) rc = make_kv_map(&mvt, a.v, a.B, kv_heads, a.N, a.d, a.v_sb, a.v_sh, a.v_sn, true, C::kBlockN);
+    if (rc != ASTRAEA_OK) return rc;
+    static PerDeviceOnce attrs;
+    if (attrs.run([] {
+            cudaError_t e = cudaFuncSetAttribute(sparse_attn_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::kSmemBytes);
+            if (e == cudaSuccess)
+                e = cudaFuncSetAttribute(sparse_attn_kernel<C>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
+            return e;
+        }) != cudaSuccess)
+        return check_launch("astraea_window_attn (shared memory attribute)");
+    WindowParams p = {};
+    p.q = reinterpret_cast<const __nv_bfloat16 *>(a.q);
+    p.q_sb = a.q_sb; p.q_sh = a.q_sh; p.q_sn = a.q_sn;
+    p.q_idx = a.q_idx; p.M = a.M;
+    p.out = reinterpret_cast<__nv_bfloat16 *>(a.out);
+    p.lse_out = a.lse_out;
+    p.N = a.N; p.H = a.H; p.N_tok = a.N_tok;
+    p.scale = a.scale;
+    p.scale_log2 = a.scale * 1.4426950408889634f;
+    p.compact = (a.flags & ASTRAEA_ATTN_COMPACT_OUT) ? 1 : 0;
+    p.err_word = a.err_word;
+    p.tiles_x = (int)(((long long)a.M * w.group + 2 * kBlockM - 1) / (2 * kBlockM));
+    p.heads = kv_heads;
+    p.group = w.group; p.left = w.left; p.right = w.right; p.n_first = w.n_first; p.last0 = a.N - w.n_last;
+    p.kv_len = w.kv_len;
+    p.q_compact = (a.flags & ASTRAEA_ATTN_COMPACT_Q) ? 1 : 0;
+    p.v = reinterpret_cast<const __nv_bfloat16 *>(a.v);
+    p.v_sb = a.v_sb; p.v_sh = a.v_sh; p.v_sn = a.v_sn;
+    const long long units = (long long)p.tiles_x * kv_heads * a.B;
+    if (units + kMaxSplitParts > 0x7fffffffll) return fail(ASTRAEA_ERR_INVALID_ARG, "astraea_window_attn: too many CTAs");
+    const SplitPlan plan = (a.flags & ASTRAEA_ATTN_WHOLE_KEYS) ? SplitPlan() : window_plan(w);
+    const bool split = plan.split > 1;
+    p.n_full = (int)units - (split ? plan.units : 0);
+    p.split = plan.split;
+    if (split) {
+        const size_t rows = (size_t)plan.units * plan.split * (2 * kBlockM);
+        p.part_lse = reinterpret_cast<float *>(static_cast<char *>(a.split_ws));
+        p.part_o = p.part_lse + (rows + 63) / 64 * 64;
+    }
+    p.n_ctas = p.n_full + (split ? plan.units * plan.split : 0);
+    launch_overlapped(sparse_attn_kernel<C>, (unsigned)p.n_ctas, C::kThreads, C::kSmemBytes, stream, mk, mv, mkt, mvt, p);
+    if (split) launch_overlapped(merge_window_kernel<DH, 2 * kBlockM>, dim3(DH / 8, plan.units), 2 * kBlockM, 0, stream, p);
+    return check_launch("astraea_window_attn");
+}
+}  // namespace
+
+int32_t launch_window_attn(const WindowArgs &w, cudaStream_t stream)
+{
+    switch (w.a.d) {
+    case 64: return launch_window_dh<64>(w, stream);
+    case 72: return launch_window_dh<72>(w, stream);
+    case 128: return launch_window_dh<128>(w, stream);
+    default: return fail(ASTRAEA_ERR_UNSUPPORTED, "head_dim %d is not supported", w.a.d);
     }
 }
 

@@ -160,6 +160,22 @@ struct AttnArgs {
     int copy_elems = 0;
 };
 int32_t launch_sparse_attn(const AttnArgs &a, cudaStream_t stream);
+// Attention over a window: the H query heads share H / group key heads; the copy and the range of heads of AttnArgs are not used.
+struct WindowArgs {
+    AttnArgs a;
+    int group, left, right, n_first, n_last;
+    const int32_t *kv_len;
+};
+int32_t launch_window_attn(const WindowArgs &w, cudaStream_t stream);
+// 256 bytes for the error word and room for the key shares of up to kMaxWindowSplit CTAs a unit (fp32 rows and LSEs of 256 rows each)
+constexpr int kMaxWindowSplit = 16;          // shares per unit: the heads of a single token are all that one (batch, key head) has
+constexpr int kMaxSplitParts = 2 * 148;      // shares per launch
+inline size_t split_bytes(long long parts, int d) { return (size_t)parts * 256 * ((size_t)d * 4 + 4) + 256; }
+inline size_t window_workspace_bytes(int B, int H, int M, int d) {
+    if (B <= 0 || H <= 0 || M <= 0 || d <= 0) return 256;
+    const long long parts = (long long)B * H * ((M + 255ll) / 256) * kMaxWindowSplit;
+    return 256 + split_bytes(parts < kMaxSplitParts ? parts : kMaxSplitParts, d);
+}
 // the schedule launch_sparse_attn would pick (host logic only; uses B, H / head_count, N, M, d, flags, split_ws, split_ws_bytes)
 void attn_plan(const AttnArgs &a, int *small_ctas, int *split_units, int *split);
 size_t attn_workspace_bytes(int B, int H, int N, int M, int d);

@@ -75,3 +75,22 @@ def test_binding_raises_and_an_empty_list_is_not_all_rows(L):
     h = A.head_rows(torch.zeros(8), (8, 8, 8), torch.zeros(8), (8, 8, 8), 1, torch.zeros(1, 0, dtype=torch.int32), 0)
     assert h.idx and h.M == 0
     assert ctypes.sizeof(A.HeadRows) == 8 * 11 + 16
+
+
+def test_window_attention(L):
+    def call(q=P, k=P, v=P, out=P, qs=(1024, 64, 128), ks=(1024, 64, 128), idx=P, M=4, kv_len=None, B=1, H=2, H_kv=2, N=16, d=64, n_first=0, n_last=0,
+             left=1, right=1, scale=0.0, flags=0, ws=P, size=256):
+        return L.astraea_window_attn(q, k, v, *qs, *ks, *ks, idx, M, kv_len, out, None, B, H, H_kv, N, d, n_first, n_last, left, right, scale, flags,
+                                     ws, size, None)
+
+    assert call(d=96) == A.ERR_UNSUPPORTED and call(flags=A.ATTN_SMALL_CTAS) == A.ERR_UNSUPPORTED and call(flags=16) == A.ERR_UNSUPPORTED
+    assert call(ws=None) == A.ERR_WORKSPACE_TOO_SMALL and call(size=255) == A.ERR_WORKSPACE_TOO_SMALL
+    for bad in (dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q=P + 8), dict(out=P + 8), dict(qs=(1024, 64, 100)), dict(ks=(1024, 60, 128)),
+                dict(qs=(1024, 64, 32)), dict(ks=(-8, 64, 128)), dict(M=17), dict(M=-1), dict(B=0), dict(H=3), dict(H_kv=0), dict(N=0), dict(N=(1 << 30) + 1),
+                dict(n_first=-1), dict(n_last=-1), dict(left=-1), dict(right=-1), dict(scale=-1.0), dict(ws=P + 128),
+                dict(N=1 << 29, M=1 << 29, H=8, H_kv=2)):
+        assert call(**bad) == A.ERR_INVALID_ARG, bad
+    assert call(M=0) == A.OK
+    # room for the key shares: one unit's at least, no more than 296 shares
+    assert 256 + 16 * 256 * 516 <= L.astraea_workspace_bytes(A.OP_WINDOW_ATTN, 1, 1, 1000, 1, 128) < 3 << 20
+    assert L.astraea_workspace_bytes(A.OP_WINDOW_ATTN, 8, 64, 1 << 20, 1 << 20, 128) < 40 << 20
