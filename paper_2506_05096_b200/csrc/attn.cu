@@ -1125,15 +1125,8 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
                 wait_bar(bar.vf + 8 * sv, ((gv0 + j) / C::kStagesV) & 1, &abort_flag, p.err_word);
                 const int k0 = key_of(j), end = key_list.end(tile0 + j);
                 if (!sees_all(k0, end, key_list.all_lo, key_list.all_hi, p.n_first, p.last0)) {
-                    uint4 *v = reinterpret_cast<uint4 *>(smem_gen + (sV - smem_base) + sv * C::kTileBytes);
-                    bool odd = false;
-                    // rows of 128 bytes in each chunk, of 32 in the tail (the swizzle keeps a row's bytes in its row)
-#pragma unroll 4
-                    for (int i = lane; i < C::kLoadBytes / 16; i += 32) {
-                        const int row = i < C::kChunks * C::kChunkBytes / 16 ? i / 8 % kBlockN : (i - C::kChunks * C::kChunkBytes / 16) / 2;
-                        const uint4 is = v[i], to = k0 + row < end ? clear_odd(is, odd) : make_uint4(0, 0, 0, 0);
-                        if (is.x != to.x || is.y != to.y || is.z != to.z || is.w != to.w) v[i] = to;
-                    }
+                    const bool odd = clean_values<C::kChunkBytes, C::kChunks, C::kLoadBytes>(
+                        reinterpret_cast<uint4 *>(smem_gen + (sV - smem_base) + sv * C::kTileBytes), end - k0, lane);
                     if (odd) *static_cast<volatile int *>(&odd_values) = 1;
                     fence_proxy_async_smem();
                 }
@@ -1669,6 +1662,14 @@ SplitPlan window_plan(const WindowArgs &a)
     const long long tiles = window_tiles(a);
     const int tail = (int)(units % n_sm);
     if (tail == 0) return plan;
+    // a stream's steps repeat a few shapes, and the estimate takes 20-150 us: the last answers are kept
+    struct Memo { long long units = -1, tiles = -1; int pairs = 0, n_sm = 0, d = 0; bool light_last = false; size_t ws = 0; SplitPlan plan; };
+    constexpr int kMemo = 16;
+    thread_local Memo memo[kMemo];
+    thread_local int memo_next = 0;
+    for (const Memo &e : memo)
+        if (e.units == units && e.tiles == tiles && e.pairs == pairs && e.light_last == light_last && e.n_sm == n_sm && e.d == a.a.d && e.ws == a.a.split_ws_bytes)
+            return e.plan;
     const double whole = finish_time(units, pairs, light_last, n_sm, 0, 1);
     double best = whole;
     for (int s = 2; s <= kMaxWindowSplit && s * 2 <= tiles; ++s) {
@@ -1676,6 +1677,9 @@ SplitPlan window_plan(const WindowArgs &a)
         const double t = finish_time(units, pairs, light_last, n_sm, tail, s, 4.0 / (double)tiles);
         if (t < 0.97 * whole && t < best) { best = t; plan.units = tail; plan.split = s; }
     }
+    Memo &e = memo[memo_next];
+    memo_next = (memo_next + 1) % kMemo;
+    e.units = units; e.tiles = tiles; e.pairs = pairs; e.light_last = light_last; e.n_sm = n_sm; e.d = a.a.d; e.ws = a.a.split_ws_bytes; e.plan = plan;
     return plan;
 }
 

@@ -15,7 +15,6 @@ namespace astraea {
 namespace {
 
 constexpr int kWarps = 4;                                          // per block
-constexpr int kUnroll = 3;                                         // heads in flight per lane: divides the steps of 24 x 128, 16 x 72, 48 x 64
 
 struct HeadTensor {
     const __nv_bfloat16 *x;
@@ -39,6 +38,7 @@ template <int DH> struct Lanes {
     static constexpr int kPiece = DH == 72 ? 4 : 8;                // channels of a lane's piece of each half
     static constexpr int kGroup = DH / 2 / kPiece;                 // lanes of a head: 4, 9, 8
     static constexpr int kHeads = 32 / kGroup;                     // heads that a warp takes at once: 8, 3, 4
+    static constexpr int kUnroll = DH == 72 ? 6 : 3;               // and how often before it waits: 96 bytes in flight per lane
 };
 
 // one piece of a head: 16 or 8 bytes
@@ -89,14 +89,25 @@ __global__ void __launch_bounds__(kWarps * 32) head_norm_kernel(const __grid_con
     grid_dependency_wait();
     int held = -1;                                                 // tensor whose weights are held
     f32x2 w[2][kPairs], bi[2][LAYER ? kPairs : 1];
-    for (int u = blockIdx.x * kWarps + warp; u < p.units; u += gridDim.x * kWarps) {
-        const int which = u >= p.units0 ? 1 : 0;
+    struct Unit { int which, row, part, b, r, tok, before; };
+    auto unit_at = [&](int u) {
+        Unit n = {};
+        if (u >= p.units) return n;
+        n.which = u >= p.units0 ? 1 : 0;
+        const HeadTensor &t = p.t[n.which];
+        const int v = n.which ? u - p.units0 : u;
+        n.row = t.parts == 1 ? v : v / t.parts; n.part = v - n.row * t.parts;
+        n.b = n.row / t.M; n.r = n.row - n.b * t.M;
+        n.tok = t.idx ? __ldcg(t.idx + n.row) : n.r;
+        n.before = (t.idx && n.r > 0) ? __ldcg(t.idx + n.row - 1) : -1;
+        return n;
+    };
+    int u = blockIdx.x * kWarps + warp;
+    Unit next = unit_at(u);                                        // list entries are fetched a token ahead
+    for (; u < p.units; u += gridDim.x * kWarps) {
+        const int which = next.which, part = next.part, b = next.b, r = next.r, tok = next.tok, before = next.before;
         const HeadTensor &t = p.t[which];
-        const int v = which ? u - p.units0 : u;
-        const int row = t.parts == 1 ? v : v / t.parts, part = v - row * t.parts;
-        const int b = row / t.M, r = row - b * t.M;
-        const int tok = t.idx ? __ldcg(t.idx + row) : r;
-        const int before = (t.idx && r > 0) ? __ldcg(t.idx + row - 1) : -1;
+        next = unit_at(u + gridDim.x * kWarps);
         if ((unsigned)tok >= (unsigned)p.N || before >= tok) {     // see astraea_scatter_reuse
             if (lane == 0 && part == 0 && p.err_word) atomicExch(p.err_word, kErrBadIndex);
             continue;
@@ -137,10 +148,10 @@ __global__ void __launch_bounds__(kWarps * 32) head_norm_kernel(const __grid_con
         const __nv_bfloat16 *src = t.x + b * t.x_sb + (int64_t)(t.compact_in ? r : tok) * t.x_sn + l * P;
         __nv_bfloat16 *dst = t.y + b * t.y_sb + (int64_t)(t.compact_out ? r : tok) * t.y_sn + l * P;
         const int h0 = part * t.part_heads, h1 = min(t.H, h0 + t.part_heads);
-        for (int hb = h0 + sub; hb - sub < h1; hb += kUnroll * L::kHeads) {
-            uint32_t raw[kUnroll][2][kPairs];
+        for (int hb = h0 + sub; hb - sub < h1; hb += L::kUnroll * L::kHeads) {
+            uint32_t raw[L::kUnroll][2][kPairs];
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
+            for (int k = 0; k < L::kUnroll; ++k) {
                 const int h = hb + k * L::kHeads;
                 if (on && h < h1) {
                     load_piece<P>(src + h * t.x_sh, raw[k][0]);
@@ -151,7 +162,7 @@ __global__ void __launch_bounds__(kWarps * 32) head_norm_kernel(const __grid_con
                 }
             }
 #pragma unroll
-            for (int k = 0; k < kUnroll; ++k) {
+            for (int k = 0; k < L::kUnroll; ++k) {
                 const int h = hb + k * L::kHeads;
                 if (h - sub >= h1) break;                          // the whole warp: no head of this step is left
                 f32x2 z[2][kPairs];

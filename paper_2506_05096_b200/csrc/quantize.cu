@@ -74,13 +74,19 @@ quantize_rows_kernel(const uint4 *__restrict__ x, const int32_t *__restrict__ id
         const uint4 *src = x + (compact_in ? t : (long long)b * N + tok) * vecs;
         uint2 *dst = xq + t * vecs;
         const int k0 = part * part_blocks, k1 = min(blocks, k0 + part_blocks);
-        for (int kb = k0; kb < k1; kb += 2 * kUnroll) {
-            uint4 v[kUnroll];
+        uint4 v[kUnroll], ahead[kUnroll];
+        auto fetch = [&](int kb) {
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
                 const int c = (kb + 2 * i) * 16 + lane;
-                v[i] = c < k1 * 16 ? ld_stream(src + c) : make_uint4(0, 0, 0, 0);
+                ahead[i] = c < k1 * 16 ? ld_stream(src + c) : make_uint4(0, 0, 0, 0);
             }
+        };
+        fetch(k0);
+        for (int kb = k0; kb < k1; kb += 2 * kUnroll) {
+#pragma unroll
+            for (int i = 0; i < kUnroll; ++i) v[i] = ahead[i];
+            if (kb + 2 * kUnroll < k1) fetch(kb + 2 * kUnroll);
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
                 const int c = (kb + 2 * i) * 16 + lane;

@@ -110,6 +110,42 @@ __device__ __forceinline__ uint4 clear_odd(uint4 v, bool &odd)
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Whether eight bf16 hold one that is not finite shows in the largest magnitude so far, NaN counting as the largest: one instruction a word.
+__device__ __forceinline__ void largest(uint32_t &m, const uint4 &v)
+{
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.x));
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.y));
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.z));
+    asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(v.w));
+}
+// A tile of values in shared memory (a row is 128 bytes in each of the chunks of CHUNK_BYTES and 32 in what is left of LOAD_BYTES behind
+// them; the swizzle keeps a row's bytes in its row) by one warp: rows from `rows` on and elements that are not finite become zero.  True if
+// there were such elements in the rows before.  Read with eight loads in flight, and written only where there is something to clear.
+template <int CHUNK_BYTES, int CHUNKS, int LOAD_BYTES>
+__device__ __forceinline__ bool clean_values(uint4 *v, int rows, int lane)
+{
+    constexpr int kVecs = LOAD_BYTES / 16, kMain = CHUNKS * CHUNK_BYTES / 16, kRound = kVecs % 256 == 0 ? 8 : kVecs % 160 == 0 ? 5 : 4;
+    static_assert(kVecs % (32 * kRound) == 0, "whole rounds");
+    auto row_of = [](int i) { return i < kMain ? i / 8 % kKeyTile : (i - kMain) / 2; };
+    bool odd = false;
+    uint32_t m = 0;
+    for (int i0 = lane; i0 < kVecs; i0 += 32 * kRound) {
+        uint4 x[kRound];
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) x[u] = v[i0 + 32 * u];
+#pragma unroll
+        for (int u = 0; u < kRound; ++u) largest(m, x[u]);
+    }
+    const bool look = (m & 0x7f80u) == 0x7f80u || (m & 0x7f800000u) == 0x7f800000u;
+    if (__any_sync(0xffffffffu, look) || rows < kKeyTile) {
+        for (int i = lane; i < kVecs; i += 32) {
+            if (row_of(i) >= rows) v[i] = make_uint4(0, 0, 0, 0);
+            else if (look) v[i] = clear_odd(v[i], odd);
+        }
+    }
+    return odd;
+}
+
 // What was cleared is put back behind the rows' epilogue, by each row's own thread and for the keys that it sees: an element of +-inf or NaN
 // times a probability above zero is that element, whatever is added to it, so it is added to the row that has been written.  Rows of
 // values that are not finite are not met in a program that works: this is slow and need not be fast.

@@ -21,6 +21,7 @@ struct __nv_bfloat16 { uint16_t b; };
 static float __bfloat162float(__nv_bfloat16 v) { uint32_t u = (uint32_t)v.b << 16; float f; memcpy(&f, &u, 4); return f; }
 template <class T> static T __ldcg(const T *p) { return *p; }
 struct Params { const int32_t *q_idx; int M, N, N_tok; };
+static bool __any_sync(unsigned, bool b) { return b; }
 #define asm(...)
 #define volatile
 #include "../paper_2506_05096_b200/csrc/window_keys.cuh"
