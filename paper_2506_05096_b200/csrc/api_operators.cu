@@ -139,7 +139,7 @@ int32_t astraea_gathered_linear_fp8(const void *xq, const float *x_scale, const 
     REQUIRE((reinterpret_cast<uintptr_t>(workspace) & 255u) == 0, "%s: workspace must be 256-byte aligned", fn);
     const long long rows = (long long)B * (idx ? M : N);
     if (rows == 0) return ASTRAEA_OK;
-    REQUIRE(rows <= 0x7fffffffll - 256, "%s: too many rows", fn);
+    REQUIRE((long long)B * N <= 0x7fffffffll - 256, "%s: too many rows", fn);
     REQUIRE((rows + 255) / 256 * ((N_out + 63) / 64) <= 0x7fffffffll, "%s: too many tiles", fn);
     REQUIRE(xq && x_scale && wq && w_scale && y, "%s: null xq, x_scale, wq, w_scale or y", fn);
     REQUIRE(aligned16(xq) && aligned16(wq) && aligned16(y) && aligned16(bias) && aligned16(residual) && aligned16(gate),

@@ -266,7 +266,6 @@ struct WindowState : SoftmaxState {
     const KeyList *keys;            // of the CTA (shared memory)
     int tile0;                      // its first key tile in that list
     int lo, hi;                     // keys in reach of this thread's row
-    int warp_lo, warp_hi;           // keys in reach of all rows of the warp
     int n_first, last0;
     bool seen;                      // some key of the CTA's tiles is visible to the row
 };
@@ -349,7 +348,8 @@ enum { kSpeculate = 0, kMaxOnly = 1, kExact = 2 };
 
 // One key tile of the softmax.  j: key tile; g: running count of S-buffer uses of this query tile (buffer
 // g % kSBufs, barrier phase (g / kSBufs) & 1), which keeps counting across the passes.
-template <class C, int MODE>
+// HIDE (windows only): some row of the warp may not see the whole tile.
+template <class C, int MODE, bool HIDE = false>
 __device__ __forceinline__ void softmax_step(StateOf<C> &st, int j, int g)
 {
     constexpr int kSBufs = C::kSBufs, NS = C::kBlockN;
@@ -357,21 +357,34 @@ __device__ __forceinline__ void softmax_step(StateOf<C> &st, int j, int g)
     const uint32_t t_s = st.t_s0 + buf * NS;
     const float sl2 = st.sl2;
     float cur[NS];
+    uint64_t visible = ~0ull;                          // keys of the tile that this row sees
+    if constexpr (HIDE) {
+        const int k0 = st.keys->key(st.tile0 + j), end = st.keys->end(st.tile0 + j);
+        visible = visible_bits(k0, end, st.lo, st.hi, st.n_first, st.last0);
+        // (the rows of a CTA lie apart: a fifth of a window's tiles are out of the reach of a whole warp)
+        if (!__any_sync(0xffffffffu, visible != 0) && !(MODE == kSpeculate && j == 0)) {
+            wait_bar(st.bar_s + 8 * buf, (g / kSBufs) & 1, st.abort_flag, st.err_word);
+            tc_fence_after();
+            if constexpr (MODE != kMaxOnly) {
+                const uint32_t zero[NS / 2] = {};
+                store_p<NS>(t_s, zero);
+                publish_p(st.bar_p + 8 * buf);
+            } else {
+                tc_fence_before();
+                mbar_arrive(st.bar_p + 8 * buf);
+            }
+            return;
+        }
+    }
+    if constexpr (C::kWindow) st.seen |= visible != 0;
     // the load is waited for at once: registers of a tcgen05.ld in flight must not be touched, and the
     // compiler cannot know that
     wait_bar(st.bar_s + 8 * buf, (g / kSBufs) & 1, st.abort_flag, st.err_word);
     tc_fence_after();
     load_s<NS>(t_s, cur);
     wait_s_regs<NS>(cur);
-    uint64_t visible = ~0ull;                          // keys of the tile that this row sees
-    bool some_hidden = false;                          // for the warp
-    if constexpr (C::kWindow) {
-        const int k0 = st.keys->key(st.tile0 + j), end = st.keys->end(st.tile0 + j);
-        some_hidden = !sees_all(k0, end, st.warp_lo, st.warp_hi, st.n_first, st.last0);
-        if (some_hidden) visible = visible_bits(k0, end, st.lo, st.hi, st.n_first, st.last0);
-        st.seen |= visible != 0;
-        if (MODE == kMaxOnly && some_hidden) hide<NS>(cur, visible, -INFINITY);
-    } else mask_tail<NS>(cur, st.N - j * NS);
+    if constexpr (HIDE && MODE == kMaxOnly) hide<NS>(cur, visible, -INFINITY);
+    if constexpr (!C::kWindow) mask_tail<NS>(cur, st.N - j * NS);
     if constexpr (MODE == kMaxOnly) {
         st.m_ref = fmaxf(st.m_ref, row_max<NS>(cur));
         tc_fence_before();
@@ -396,7 +409,7 @@ __device__ __forceinline__ void softmax_step(StateOf<C> &st, int j, int g)
             cur[i] = ex2(cur[i]); cur[i + 1] = ex2(cur[i + 1]);
         }
     }
-    if constexpr (C::kWindow) { if (some_hidden) hide<NS>(cur, visible, 0.f); }
+    if constexpr (HIDE) hide<NS>(cur, visible, 0.f);
     float tile_sum = 0.f;
     if constexpr (!C::kOnes) {
         unsigned long long a[4] = {0ull, 0ull, 0ull, 0ull};
@@ -514,10 +527,22 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
         st.keys = keys; st.tile0 = tile0;
         st.n_first = p.n_first; st.last0 = p.last0;
         st.lo = tok - p.left; st.hi = tok + p.right;
-        st.warp_lo = __reduce_max_sync(0xffffffffu, tok >= 0 ? st.lo : INT_MIN);
-        st.warp_hi = __reduce_min_sync(0xffffffffu, tok >= 0 ? st.hi : INT_MAX);
         st.seen = false;
     }
+    // a pass over this warpgroup's key tiles
+    auto run_pass = [&](auto mode, int g0) {
+        constexpr int MODE = decltype(mode)::value;
+        if constexpr (C::kWindow) {
+            const WholeTiles whole = whole_tiles(*keys, __reduce_max_sync(0xffffffffu, tok >= 0 ? st.lo : INT_MIN),
+                                                 __reduce_min_sync(0xffffffffu, tok >= 0 ? st.hi : INT_MAX), p.n_first, p.last0);
+            for (int j = par; j < n_tiles; j += kSplit) {
+                if (whole.has(tile0 + j)) softmax_step<C, MODE>(st, j, g0 + j);
+                else softmax_step<C, MODE, true>(st, j, g0 + j);
+            }
+        } else {
+            for (int j = par; j < n_tiles; j += kSplit) softmax_step<C, MODE>(st, j, g0 + j);
+        }
+    };
     st.m_ref = -INFINITY;
     st.shift = kRefShift;
     const bool no_keys = C::kWindow && n_tiles == 0;
@@ -527,7 +552,7 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
         else asm volatile("bar.sync 4, 256;" ::: "memory");
         st.m_ref = *st.ref_x;
     }
-    for (int j = par; j < n_tiles; j += kSplit) softmax_step<C, kSpeculate>(st, j, j);
+    run_pass(std::integral_constant<int, kSpeculate>(), 0);
     if (!no_keys) wait_bar(st.bar_done, 0, abort_flag, p.err_word);            // every P V of this query tile has landed
     if constexpr (C::kWindow) {
         // The reference is the largest logit of the first key tile, seen or not: where all that the row sees lies far below it, small
@@ -552,7 +577,7 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
     if (*redo_flag) {
         // a tile overflowed somewhere in the CTA: exact row maxima first, then the whole pass again
         st.m_ref = -INFINITY;
-        for (int j = par; j < n_tiles; j += kSplit) softmax_step<C, kMaxOnly>(st, j, n_tiles + j);
+        run_pass(std::integral_constant<int, kMaxOnly>(), n_tiles);
         xchg[wtid + par * kBlockM].x = st.m_ref;
         if (tile == 0) asm volatile("bar.sync 1, 256;" ::: "memory");
         else asm volatile("bar.sync 2, 256;" ::: "memory");
@@ -560,7 +585,7 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
         if (C::kWindow && st.m_ref == -INFINITY) st.m_ref = 0.f;  // nothing that counts is seen: all terms are 0 against any reference
         st.shift = 0.f;
         st.l_sum = 0.f;
-        for (int j = par; j < n_tiles; j += kSplit) softmax_step<C, kExact>(st, j, 2 * n_tiles + j);
+        run_pass(std::integral_constant<int, kExact>(), 2 * n_tiles);
         wait_bar(st.bar_done, 1, abort_flag, p.err_word);
         if constexpr (C::kOnes) {
             tc_fence_after();
@@ -1119,12 +1144,13 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsOther));
         // ------------------------------------------------ looks at the values of a stage before the MMAs (see clear_odd)
         const int lane = tid & 31;
+        const WholeTiles whole = whole_tiles(key_list, key_list.all_lo, key_list.all_hi, p.n_first, p.last0);
         auto look_pass = [&](int gv0) {
             for (int j = 0; j < n_tiles; ++j) {
                 const int sv = (gv0 + j) % C::kStagesV;
                 wait_bar(bar.vf + 8 * sv, ((gv0 + j) / C::kStagesV) & 1, &abort_flag, p.err_word);
-                const int k0 = key_of(j), end = key_list.end(tile0 + j);
-                if (!sees_all(k0, end, key_list.all_lo, key_list.all_hi, p.n_first, p.last0)) {
+                if (!whole.has(tile0 + j)) {
+                    const int k0 = key_of(j), end = key_list.end(tile0 + j);
                     const bool odd = clean_values<C::kChunkBytes, C::kChunks, C::kLoadBytes>(
                         reinterpret_cast<uint4 *>(smem_gen + (sV - smem_base) + sv * C::kTileBytes), end - k0, lane);
                     if (odd) *static_cast<volatile int *>(&odd_values) = 1;

@@ -5,9 +5,10 @@
 // (Section 3.2: such layers act on every token by itself, so queries are needed for the selected tokens only; keys for all).
 //
 // HBM-bound: every value is read once and written once, in one launch for queries and keys.  A warp takes one token's heads (a share of
-// them in short launches); its cosines and sines, 4 d bytes, are read once for all of them, weights once per warp.  A lane owns the same
-// piece of the first and of the second half of a head (16 bytes each; 8 at head_dim 72, whose halves are 72 bytes), so that both ways of
-// pairing channels, (2p, 2p + 1) and (p, p + d/2), stay inside a lane and only the sums of the norm go round: over 4, 9 or 8 lanes.
+// them in short launches); what weights, cosines and sines make of a channel pair is two products and a sum, whose factors are computed
+// once per token and used for all of its heads.  A lane owns the same channels of the first and of the second half of a head (16 bytes
+// each; three times 8 bytes at head_dim 72, whose halves are 72 bytes), so that both ways of pairing channels, (2p, 2p + 1) and
+// (p, p + d/2), stay inside a lane and only the sums of the norm go round: over 4, 3 or 8 lanes.
 // fp32 arithmetic, one rounding to bf16 at the end.
 #include "common.cuh"
 
@@ -34,41 +35,52 @@ struct HeadNormParams {
     int *err_word;
 };
 
-template <int DH> struct Lanes {
-    static constexpr int kPiece = DH == 72 ? 4 : 8;                // channels of a lane's piece of each half
-    static constexpr int kGroup = DH / 2 / kPiece;                 // lanes of a head: 4, 9, 8
-    static constexpr int kHeads = 32 / kGroup;                     // heads that a warp takes at once: 8, 3, 4
-    static constexpr int kUnroll = DH == 72 ? 6 : 3;               // and how often before it waits: 96 bytes in flight per lane
+template <int DH, bool LAYER = false> struct Lanes {
+    static constexpr int kUnit = DH == 72 ? 4 : 8;                 // channels of one access
+    static constexpr int kUnits = DH == 72 ? 3 : 1;                // accesses of a lane to each half of a head
+    static constexpr int kGroup = DH / 2 / (kUnit * kUnits);       // lanes of a head: 4, 3, 8
+    static constexpr int kHeads = 32 / kGroup;                     // heads that a warp takes at once: 8, 10, 4
+    static constexpr int kUnroll = DH == 72 ? 2 : LAYER ? 3 : 6;              // and how often before it waits (24 x 128, 16 x 72, 48 x 64 are one round)
 };
 
-// one piece of a head: 16 or 8 bytes
-template <int P> __device__ __forceinline__ void load_piece(const __nv_bfloat16 *p, uint32_t (&r)[P / 2]) {
-    if constexpr (P == 8) {
+// one access to a head: 16 or 8 bytes
+template <int U> __device__ __forceinline__ void load_unit(const __nv_bfloat16 *p, uint32_t *r) {
+    if constexpr (U == 8) {
         const uint4 v = ld_stream(reinterpret_cast<const uint4 *>(p));
         r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w;
     } else asm volatile("ld.global.v2.u32 {%0,%1}, [%2];" : "=r"(r[0]), "=r"(r[1]) : "l"(p));
 }
-template <int P> __device__ __forceinline__ void store_piece(__nv_bfloat16 *p, const f32x2 (&f)[P / 2]) {
-    uint32_t w[P / 2];
+template <int U> __device__ __forceinline__ void store_unit(__nv_bfloat16 *p, const f32x2 *f) {
+    uint32_t w[U / 2];
 #pragma unroll
-    for (int i = 0; i < P / 2; ++i) {
+    for (int i = 0; i < U / 2; ++i) {
         float lo, hi;
         unpack2(f[i], lo, hi);
         __nv_bfloat162 v2 = __floats2bfloat162_rn(lo, hi);
         w[i] = *reinterpret_cast<uint32_t *>(&v2);
     }
-    if constexpr (P == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    if constexpr (U == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
 }
+// N consecutive values of a table
+template <int N> __device__ __forceinline__ void load_table(const float *p, float *f) {
+    if constexpr (N == 2) asm volatile("ld.global.v2.f32 {%0,%1}, [%2];" : "=f"(f[0]), "=f"(f[1]) : "l"(p));
+    else {
+#pragma unroll
+        for (int i = 0; i < N; i += 4)
+            asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f[i]), "=f"(f[i + 1]), "=f"(f[i + 2]), "=f"(f[i + 3]) : "l"(p + i));
+    }
+}
 __device__ __forceinline__ f32x2 widen(uint32_t w) { return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ f32x2 swapped(uint32_t w) { return pack2(__uint_as_float(w & 0xffff0000u), __uint_as_float(w << 16)); }
+__device__ __forceinline__ f32x2 swapped(f32x2 v) { float lo, hi; unpack2(v, lo, hi); return pack2(hi, lo); }
 __device__ __forceinline__ f32x2 twice(float v) { return pack2(v, v); }
 
 // the sum over the lanes of a head
 template <int G> __device__ __forceinline__ float group_sum(float s, int lane) {
-    if constexpr (G == 9) {
-        const int base = lane / 9 * 9, l = lane - base;            // lanes 27..31 hold no head: their sums are not used
-        const float t = s + __shfl_sync(0xffffffffu, s, base + (l + 3) % 9) + __shfl_sync(0xffffffffu, s, base + (l + 6) % 9);
-        return t + __shfl_sync(0xffffffffu, t, base + (l + 1) % 9) + __shfl_sync(0xffffffffu, t, base + (l + 2) % 9);
+    if constexpr (G == 3) {
+        const int l = lane % 3, base = lane - l;                   // lanes 30 and 31 hold no head: their sums are not used
+        return s + __shfl_sync(0xffffffffu, s, base + (l + 1) % 3) + __shfl_sync(0xffffffffu, s, base + (l + 2) % 3);
     } else {
 #pragma unroll
         for (int o = G / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
@@ -78,17 +90,15 @@ template <int G> __device__ __forceinline__ float group_sum(float s, int lane) {
 
 // LAYER: layer norm with a bias (RMS norm without one otherwise); HALF: channels are paired (p, p + DH/2) and not (2p, 2p + 1)
 template <int DH, bool LAYER, bool HALF>
-__global__ void __launch_bounds__(kWarps * 32) head_norm_kernel(const __grid_constant__ HeadNormParams p)
+__global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_norm_kernel(const __grid_constant__ HeadNormParams p)
 {
-    using L = Lanes<DH>;
-    constexpr int P = L::kPiece, G = L::kGroup, kPairs = P / 2;
+    using L = Lanes<DH, LAYER>;
+    constexpr int U = L::kUnit, G = L::kGroup, kPairs = L::kUnits * U / 2;      // (f32x2 pairs of a half)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int sub = lane / G, l = lane - sub * G;                  // head of the warp's kHeads, piece of the head
+    const int sub = lane / G, l = lane - sub * G;                  // head of the warp's kHeads, lane of the head
     const bool on = sub < L::kHeads;
     grid_launch_dependents();
     grid_dependency_wait();
-    int held = -1;                                                 // tensor whose weights are held
-    f32x2 w[2][kPairs], bi[2][LAYER ? kPairs : 1];
     struct Unit { int which, row, part, b, r, tok, before; };
     auto unit_at = [&](int u) {
         Unit n = {};
@@ -112,55 +122,80 @@ __global__ void __launch_bounds__(kWarps * 32) head_norm_kernel(const __grid_con
             if (lane == 0 && part == 0 && p.err_word) atomicExch(p.err_word, kErrBadIndex);
             continue;
         }
-        if (which != held) {
-            held = which;
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-#pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    const int c = s * (DH / 2) + l * P + 2 * i;
-                    const uint32_t one = 0x3F803F80u;
-                    w[s][i] = widen(on && t.weight ? *reinterpret_cast<const volatile uint32_t *>(t.weight + c) : one);
-                    if (LAYER) bi[s][LAYER ? i : 0] = widen(on && t.bias ? *reinterpret_cast<const volatile uint32_t *>(t.bias + c) : 0u);
-                }
-        }
-        // angles: HALF: of channels l P .. of the first half, as many as the piece has channels; else those of the pairs of both pieces
-        float co[P], si[P];
-        if (on && tok < p.n_rot) {
-            const float *pc = p.cos + (size_t)tok * (DH / 2), *ps = p.sin + (size_t)tok * (DH / 2);
-            auto get = [&](const float *src, float (&dst)[P]) {
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const float *a = src + (HALF ? l * P + s * kPairs : s * (DH / 4) + l * kPairs);
-                    if constexpr (P == 8) {
-                        float4 f;
-                        asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "l"(a));
-                        dst[s * 4] = f.x; dst[s * 4 + 1] = f.y; dst[s * 4 + 2] = f.z; dst[s * 4 + 3] = f.w;
-                    } else asm volatile("ld.global.v2.f32 {%0,%1}, [%2];" : "=f"(dst[s * 2]), "=f"(dst[s * 2 + 1]) : "l"(a));
-                }
-            };
-            get(pc, co);
-            get(ps, si);
-        } else {
-#pragma unroll
-            for (int i = 0; i < P; ++i) { co[i] = 1.f; si[i] = 0.f; }
-        }
-        const __nv_bfloat16 *src = t.x + b * t.x_sb + (int64_t)(t.compact_in ? r : tok) * t.x_sn + l * P;
-        __nv_bfloat16 *dst = t.y + b * t.y_sb + (int64_t)(t.compact_out ? r : tok) * t.y_sn + l * P;
+        const __nv_bfloat16 *src = t.x + b * t.x_sb + (int64_t)(t.compact_in ? r : tok) * t.x_sn + l * U;
+        __nv_bfloat16 *dst = t.y + b * t.y_sb + (int64_t)(t.compact_out ? r : tok) * t.y_sn + l * U;
         const int h0 = part * t.part_heads, h1 = min(t.H, h0 + t.part_heads);
-        for (int hb = h0 + sub; hb - sub < h1; hb += L::kUnroll * L::kHeads) {
-            uint32_t raw[L::kUnroll][2][kPairs];
+        // the first round of heads is sent for before the tables are
+        uint32_t raw[L::kUnroll][2][kPairs];
+        auto fetch = [&](int hb) {
 #pragma unroll
             for (int k = 0; k < L::kUnroll; ++k) {
                 const int h = hb + k * L::kHeads;
                 if (on && h < h1) {
-                    load_piece<P>(src + h * t.x_sh, raw[k][0]);
-                    load_piece<P>(src + h * t.x_sh + DH / 2, raw[k][1]);
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int j = 0; j < L::kUnits; ++j) load_unit<U>(src + h * t.x_sh + s * (DH / 2) + G * j * U, &raw[k][s][j * (U / 2)]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) raw[k][0][i] = raw[k][1][i] = 0u;
                 }
             }
+        };
+        fetch(h0 + sub);
+        // y = r (x by + x' cross) + plus for channel pairs x and their partners x': by = weight cos, cross = -+ partner's weight sin
+        f32x2 by[2][kPairs], cross[2][kPairs], plus[2][LAYER ? kPairs : 1];
+        {
+            const bool turned = on && tok < p.n_rot;
+            const float *pc = p.cos + (size_t)(turned ? tok : 0) * (DH / 2), *ps = p.sin + (size_t)(turned ? tok : 0) * (DH / 2);
+#pragma unroll
+            for (int j = 0; j < L::kUnits; ++j) {
+                const int c0 = (l + G * j) * U;                    // first channel of the access, in its half
+                uint32_t ww[2][U / 2], wb[2][U / 2];
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                    for (int i = 0; i < U / 2; ++i) { ww[s][i] = 0x3F803F80u; wb[s][i] = 0u; }
+                    if (on && t.weight) load_unit<U>(t.weight + s * (DH / 2) + c0, ww[s]);
+                    if (LAYER && on && t.bias) load_unit<U>(t.bias + s * (DH / 2) + c0, wb[s]);
+                }
+                float co[U], si[U];                                // HALF: of the channels; else of the pairs of both halves
+#pragma unroll
+                for (int i = 0; i < U; ++i) { co[i] = 1.f; si[i] = 0.f; }
+                if (turned) {
+                    if (HALF) { load_table<U>(pc + c0, co); load_table<U>(ps + c0, si); }
+                    else {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            load_table<U / 2>(pc + s * (DH / 4) + c0 / 2, co + s * (U / 2));
+                            load_table<U / 2>(ps + s * (DH / 4) + c0 / 2, si + s * (U / 2));
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < U / 2; ++i) {
+                    const int k = j * (U / 2) + i;
+                    if (HALF) {
+                        const f32x2 c = pack2(co[2 * i], co[2 * i + 1]), n = pack2(si[2 * i], si[2 * i + 1]), m = pack2(-si[2 * i], -si[2 * i + 1]);
+                        by[0][k] = mul2(widen(ww[0][i]), c); cross[0][k] = mul2(widen(ww[1][i]), m);
+                        by[1][k] = mul2(widen(ww[1][i]), c); cross[1][k] = mul2(widen(ww[0][i]), n);
+                        if (LAYER) {
+                            plus[0][LAYER ? k : 0] = fma2(widen(wb[0][i]), c, mul2(widen(wb[1][i]), m));
+                            plus[1][LAYER ? k : 0] = fma2(widen(wb[1][i]), c, mul2(widen(wb[0][i]), n));
+                        }
+                    } else {
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) {
+                            const f32x2 c = twice(co[s * (U / 2) + i]), n = pack2(-si[s * (U / 2) + i], si[s * (U / 2) + i]);
+                            by[s][k] = mul2(widen(ww[s][i]), c); cross[s][k] = mul2(swapped(ww[s][i]), n);
+                            if (LAYER) plus[s][LAYER ? k : 0] = fma2(widen(wb[s][i]), c, mul2(swapped(wb[s][i]), n));
+                        }
+                    }
+                }
+            }
+        }
+        for (int hb = h0 + sub; hb - sub < h1; hb += L::kUnroll * L::kHeads) {
+            if (hb != h0 + sub) fetch(hb);
 #pragma unroll
             for (int k = 0; k < L::kUnroll; ++k) {
                 const int h = hb + k * L::kHeads;
@@ -188,33 +223,18 @@ __global__ void __launch_bounds__(kWarps * 32) head_norm_kernel(const __grid_con
                 unpack2(a, lo, hi);
                 const f32x2 rstd = twice(rsqrtf(group_sum<G>(lo + hi, lane) * (1.0f / DH) + p.eps));
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+                for (int i = 0; i < kPairs; ++i) {
+                    const f32x2 x0 = z[0][i], x1 = z[1][i];
+                    z[0][i] = fma2(x0, by[0][i], mul2(HALF ? x1 : swapped(x0), cross[0][i]));
+                    z[1][i] = fma2(x1, by[1][i], mul2(HALF ? x0 : swapped(x1), cross[1][i]));
 #pragma unroll
-                    for (int i = 0; i < kPairs; ++i) {
-                        z[s][i] = mul2(z[s][i], rstd);
-                        z[s][i] = LAYER ? fma2(z[s][i], w[s][i], bi[s][LAYER ? i : 0]) : mul2(z[s][i], w[s][i]);
-                    }
-                if (HALF) {
-#pragma unroll
-                    for (int i = 0; i < kPairs; ++i) {
-                        const f32x2 c2 = pack2(co[2 * i], co[2 * i + 1]), s2 = pack2(si[2 * i], si[2 * i + 1]), m2 = pack2(-si[2 * i], -si[2 * i + 1]);
-                        const f32x2 a0 = z[0][i], a1 = z[1][i];
-                        z[0][i] = fma2(a0, c2, mul2(a1, m2));
-                        z[1][i] = fma2(a1, c2, mul2(a0, s2));
-                    }
-                } else {
+                    for (int s = 0; s < 2; ++s) z[s][i] = LAYER ? fma2(z[s][i], rstd, plus[s][LAYER ? i : 0]) : mul2(z[s][i], rstd);
+                }
+                if (on && h < h1) {
 #pragma unroll
                     for (int s = 0; s < 2; ++s)
 #pragma unroll
-                        for (int i = 0; i < kPairs; ++i) {
-                            unpack2(z[s][i], lo, hi);
-                            const float c = co[s * kPairs + i], n = si[s * kPairs + i];
-                            z[s][i] = fma2(z[s][i], twice(c), mul2(pack2(hi, lo), pack2(-n, n)));
-                        }
-                }
-                if (on && h < h1) {
-                    store_piece<P>(dst + h * t.y_sh, z[0]);
-                    store_piece<P>(dst + h * t.y_sh + DH / 2, z[1]);
+                        for (int j = 0; j < L::kUnits; ++j) store_unit<U>(dst + h * t.y_sh + s * (DH / 2) + G * j * U, &z[s][j * (U / 2)]);
                 }
             }
         }

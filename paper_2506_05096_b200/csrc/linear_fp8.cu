@@ -7,13 +7,19 @@
 // Layout of the launch as in linear.cu: persistent CTA pairs on 256-row x BN-column tiles, tcgen05.mma.cta_group::2 (kind::f8f6f4,
 // 256 x BN x 32), rows of x (always one contiguous matrix: the quantiser has gathered them) and W by TMA, one pipeline stage being one
 // block of 128 channels = 128 bytes, rows of y scattered by the epilogue.  What differs is where the sum lives: every block gets an
-// accumulator of its own in TMEM (512 / BN of them, in turn), and sixteen warps read it, scale it and add it to their registers while the
-// tensor cores are at the next blocks.  Four MMAs of a block at BN = 256 take 512 clocks of the tensor pipe; reading its 128 x 256 values
-// and the 16384 packed FMAs on them take half the issue slots of that time.  (A sum over blocks in the tensor cores would need the scales
-// to be powers of two.)
+// accumulator of its own in TMEM (two in turn at BN = 256), and eight warps read it, scale it and add it to their registers while the
+// tensor cores are at the next block.  (A sum over blocks in the tensor cores would need the scales to be powers of two.)
+//
+// At BN = 256 the MMAs of a block take 512 clocks and its 32768 FMAs half the FMA pipe's time.  What is scarce is the round trip of an
+// accumulator (512 of MMAs, 234 from their end to the warps that wait for it, the reads, 143 for the arrival at the other CTA) and the
+// issue slots of the warps that do all this, so: eight warps of 128 columns and not sixteen of 64 (the loop around the FMAs is paid half
+// as often), loads of 64 columns, the accumulator released when the last load has landed and before its FMAs, descriptors and phases
+// counted on, not computed, scales fetched four blocks ahead.  16384 x 6144 x 6144: 588 -> 413 us on zeros (clocks at their maximum), 503 us =
+// 2.46 PFLOP/s on random codes, where the power cap takes the clocks to 1.6 GHz.  (128-column tiles by two sets of warps in turn, whose epilogues
+// overlap, are slower: an MMA of 128 columns takes 80 clocks of the 64 that it should, and a commit for each block more.)
 // Warp roles of each CTA:
-//   warps 0-15  sums and epilogue: a thread has one row (TMEM lane) and BN / 4 columns; a warp's columns share the scale of W;
-//   warp 16     TMA producer, warp 17 (even CTA) MMA issuer for the pair; warps 18-19 only give their registers away.
+//   warps 0-7  sums and epilogue: a thread has one row (TMEM lane) and BN / 2 columns, which share the scale of W;
+//   warp 8     TMA producer, warp 9 (even CTA) MMA issuer for the pair; warps 10-11 only give their registers away.
 // Every mbarrier wait is bounded, and a CTA that gives up leaves as described in linear.cu.
 #include "common.cuh"
 #include "sm100_ptx.cuh"
@@ -26,20 +32,21 @@ namespace {
 using namespace ptx;
 
 constexpr int kTileRows = 256, kRowsCta = kTileRows / 2, kBK = 128;    // bytes = channels of a stage, and of a scale
-constexpr int kSumWarps = 16;
+constexpr int kSumWarps = 8;
 constexpr int kTmaWarp = kSumWarps, kMmaWarp = kTmaWarp + 1;
 constexpr int kThreads = (kSumWarps + 4) * 32;
 constexpr int kStages = 6;
 constexpr int kABytes = kRowsCta * kBK, kBBytes = 128 * kBK;           // (B: half of at most 256 columns)
 constexpr int kStageBytes = 32 * 64;                                   // per sum warp: 32 rows x 32 bf16 columns on their way to / from global memory
 constexpr int kMaxAcc = 4;
+constexpr int kAhead = 4;                                              // blocks between the load of a row's scale and its use
 constexpr int kBarBytes = 256;
 static_assert(8 * (2 * kStages + 2 * kMaxAcc + 1) <= kBarBytes, "barrier area too small");
 constexpr int kSmemBytes = kStages * (kABytes + kBBytes) + kBarBytes + kSumWarps * kStageBytes + 1024;
 static_assert(kSmemBytes + 512 <= 227 * 1024, "shared memory of one CTA");
 constexpr uint32_t kTmemCols = 512;
-// registers: 64 sums, 32 values on their way out of TMEM and the addresses of a sum warp against 96 a thread at launch
-constexpr int kRegsLaunch = 65536 / kThreads / 8 * 8, kRegsSum = 112, kRegsOther = 32;
+// registers: 128 sums, 64 values on their way out of TMEM and the addresses of a sum warp against 168 a thread at launch
+constexpr int kRegsLaunch = 65536 / kThreads / 8 * 8, kRegsSum = 232, kRegsOther = 40;
 static_assert(kRegsSum * kSumWarps * 32 + kRegsOther * 128 <= kRegsLaunch * kThreads, "setmaxnreg budget");
 
 struct Fp8Params {
@@ -52,27 +59,59 @@ struct Fp8Params {
     int *err_word;
 };
 
-// columns [col, col + 32) or [col, col + 16) of an accumulator
-template <int C> __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t (&r)[C]) {
-    if constexpr (C == 32) tmem_ld32(taddr, r); else tmem_ld16(taddr, r);
+// C columns of an accumulator, waited for, as pairs.  (One piece of assembly: as single registers that the wait then names, the values were
+// moved about before the FMAs, 85 moves for 64 of them, which took the loop from 440 to 590 us for 16384 x 6144 x 6144.)
+template <int C> __device__ __forceinline__ void load_pairs(uint32_t t, f32x2 (&a)[C / 2]);
+template <> __device__ __forceinline__ void load_pairs<32>(uint32_t t, f32x2 (&a)[16]) {
+    asm volatile("{\n\t.reg .b32 t<32>;\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {t0,t1,t2,t3,t4,t5,t6,t7,t8,t9,t10,t11,t12,t13,t14,t15,t16,t17,t18,t19,t20,t21,t22,t23,t24,t25,t26,t27,t28,t29,t30,t31}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;\n\t"
+        "mov.b64 %0, {t0,t1}; mov.b64 %1, {t2,t3}; mov.b64 %2, {t4,t5}; mov.b64 %3, {t6,t7}; mov.b64 %4, {t8,t9}; mov.b64 %5, {t10,t11}; mov.b64 %6, {t12,t13}; mov.b64 %7, {t14,t15};"
+        "mov.b64 %8, {t16,t17}; mov.b64 %9, {t18,t19}; mov.b64 %10, {t20,t21}; mov.b64 %11, {t22,t23}; mov.b64 %12, {t24,t25}; mov.b64 %13, {t26,t27}; mov.b64 %14, {t28,t29}; mov.b64 %15, {t30,t31};"
+        "}"
+        : "=l"(a[0]), "=l"(a[1]), "=l"(a[2]), "=l"(a[3]), "=l"(a[4]), "=l"(a[5]), "=l"(a[6]), "=l"(a[7]),
+          "=l"(a[8]), "=l"(a[9]), "=l"(a[10]), "=l"(a[11]), "=l"(a[12]), "=l"(a[13]), "=l"(a[14]), "=l"(a[15])
+        : "r"(t) : "memory");
+}
+template <> __device__ __forceinline__ void load_pairs<64>(uint32_t t, f32x2 (&a)[32]) {
+    asm volatile("{\n\t.reg .b32 t<64>;\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x64.b32 {t0,t1,t2,t3,t4,t5,t6,t7,t8,t9,t10,t11,t12,t13,t14,t15,t16,t17,t18,t19,t20,t21,t22,t23,t24,t25,t26,t27,t28,t29,t30,t31,t32,t33,t34,t35,t36,t37,t38,t39,t40,t41,t42,t43,t44,t45,t46,t47,t48,t49,t50,t51,t52,t53,t54,t55,t56,t57,t58,t59,t60,t61,t62,t63}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;\n\t"
+        "mov.b64 %0, {t0,t1}; mov.b64 %1, {t2,t3}; mov.b64 %2, {t4,t5}; mov.b64 %3, {t6,t7}; mov.b64 %4, {t8,t9}; mov.b64 %5, {t10,t11}; mov.b64 %6, {t12,t13}; mov.b64 %7, {t14,t15};"
+        "mov.b64 %8, {t16,t17}; mov.b64 %9, {t18,t19}; mov.b64 %10, {t20,t21}; mov.b64 %11, {t22,t23}; mov.b64 %12, {t24,t25}; mov.b64 %13, {t26,t27}; mov.b64 %14, {t28,t29}; mov.b64 %15, {t30,t31};"
+        "mov.b64 %16, {t32,t33}; mov.b64 %17, {t34,t35}; mov.b64 %18, {t36,t37}; mov.b64 %19, {t38,t39}; mov.b64 %20, {t40,t41}; mov.b64 %21, {t42,t43}; mov.b64 %22, {t44,t45}; mov.b64 %23, {t46,t47};"
+        "mov.b64 %24, {t48,t49}; mov.b64 %25, {t50,t51}; mov.b64 %26, {t52,t53}; mov.b64 %27, {t54,t55}; mov.b64 %28, {t56,t57}; mov.b64 %29, {t58,t59}; mov.b64 %30, {t60,t61}; mov.b64 %31, {t62,t63};"
+        "}"
+        : "=l"(a[0]), "=l"(a[1]), "=l"(a[2]), "=l"(a[3]), "=l"(a[4]), "=l"(a[5]), "=l"(a[6]), "=l"(a[7]),
+          "=l"(a[8]), "=l"(a[9]), "=l"(a[10]), "=l"(a[11]), "=l"(a[12]), "=l"(a[13]), "=l"(a[14]), "=l"(a[15]),
+          "=l"(a[16]), "=l"(a[17]), "=l"(a[18]), "=l"(a[19]), "=l"(a[20]), "=l"(a[21]), "=l"(a[22]), "=l"(a[23]),
+          "=l"(a[24]), "=l"(a[25]), "=l"(a[26]), "=l"(a[27]), "=l"(a[28]), "=l"(a[29]), "=l"(a[30]), "=l"(a[31])
+        : "r"(t) : "memory");
 }
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *m, uint32_t bar, int c0, int c1) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
         ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
-// one output row: of a [B, N, *] tensor, or -1 (past the end, an entry out of range or not ascending)
-__device__ __forceinline__ long long target_row(const Fp8Params &p, long long g, long long total, int *batch, bool *bad) {
-    *bad = false;
-    if (g >= total) return -1;
-    const int b = (int)((unsigned)g / (unsigned)p.M), r = (int)((unsigned)g - (unsigned)b * (unsigned)p.M);
-    const int tok = p.idx ? __ldcg(p.idx + g) : r;
-    const int before = (p.idx && r > 0) ? __ldcg(p.idx + g - 1) : -1;
-    if ((unsigned)tok >= (unsigned)p.N || (r > 0 && before >= tok)) { *bad = true; return -1; }
-    *batch = b;
-    return (long long)b * p.N + tok;
+// gelu2 with one reciprocal for both elements, of the product of their divisors (1 .. 3 with |z| limited to 6, where the erf is one): three
+// XU operations a pair instead of four, which cost an epilogue more than anything else (13106 x 1152 x 4608: 80 us without the GELU, 110 with).
+__device__ __forceinline__ f32x2 gelu2_one_reciprocal(f32x2 x) {
+    float x0, x1, d0, d1, a0, a1, r, e0, e1;
+    unpack2(x, x0, x1);
+    const f32x2 az = pack2(fminf(fabsf(x0) * 0.70710678118654752f, 6.0f), fminf(fabsf(x1) * 0.70710678118654752f, 6.0f));       // |z|
+    unpack2(fma2(az, both(0.3275911f), both(1.0f)), d0, d1);
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
+    unpack2(mul2(mul2(az, az), both(-1.4426950408889634f)), a0, a1);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(a0));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(a1));
+    const f32x2 t = pack2(r * d1, r * d0);
+    f32x2 pl = fma2(both(-0.5f * 1.061405429f), t, both(0.5f * 1.453152027f));           // minus half the polynomial
+    pl = fma2(pl, t, both(-0.5f * 1.421413741f));
+    pl = fma2(pl, t, both(0.5f * 0.284496736f));
+    pl = fma2(pl, t, both(-0.5f * 0.254829592f));
+    const f32x2 half_erf = fma2(mul2(pl, t), pack2(e0, e1), both(0.5f));                // of |z|
+    return mul2(x, add2(both(0.5f), (half_erf & 0x7fffffff7fffffffull) | (x & 0x8000000080000000ull)));
 }
-
 enum { kNothing = 0, kGelu = 1, kAnything = 2 };                       // as in linear.cu
 
 template <int BN, int EPI>
@@ -80,8 +119,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ Fp8Params p)
 {
     constexpr int kAcc = 512 / BN < kMaxAcc ? 512 / BN : kMaxAcc;      // accumulators in turn
-    constexpr int kCols = BN / 4;                                      // columns of a sum warp
-    constexpr int kChunk = kCols < 32 ? kCols : 32, kChunks = kCols / kChunk;
+    constexpr int kCols = BN / 2;                                      // columns of a sum warp
+    constexpr int kLoad = kCols < 64 ? kCols : 64;                     // columns of a load
+    constexpr int kChunk = 32, kChunks = kCols / kChunk;               // and of a step of the epilogue
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
@@ -129,75 +169,93 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + c0;
         uint8_t *stage = smem_raw + (bars + kBarBytes - smem_u32(smem_raw)) + warp * kStageBytes;
         const uint32_t s_stage = smem_u32(stage);
-        // a thread owns a row of the tile, and global memory is touched in 16-byte pieces: piece q of rows r0 + kStep j (see linear.cu)
-        constexpr int kPieces = kChunk / 8, kStep = 32 / kPieces, kRowBytes = kChunk * 2;
+        // A thread owns a row of the tile, and global memory is touched in 16-byte pieces: piece q of rows r0 + kStep j (see linear.cu; a bulk
+        // copy of each row's 64 bytes instead, by its own thread, took 1.4 times as long for 13106 x 1152 x 4608)
+        constexpr int kPieces = kChunk / 8, kStep = 32 / kPieces;
         const int q = lane % kPieces, r0 = lane / kPieces;
-        auto swizzled = [](int r, int piece) { return r * kRowBytes + ((piece ^ ((r >> (kPieces == 4 ? 1 : 2)) & (kPieces - 1))) << 4); };
-        int g = 0;
+        auto swizzled = [](int r, int piece) { return r * (kChunk * 2) + ((piece ^ ((kPieces == 8 ? r : r >> 1) & (kPieces - 1))) << 4); };
+        int acc = 0;
+        uint32_t acc_phase = 0;
+        // What a tile needs before its first block: the list's entries for its rows, the scales of the first blocks.  They are fetched in
+        // front of the epilogue of the tile before (behind it, they were 1500 clocks of every tile).
+        int tok = 0, before = -1;
+        float xs_next[kAhead], ws_lane = 0.f;                          // scales of the row, kAhead blocks ahead (an L2 round trip is longer than a block)
+        auto fetch = [&](int tile) {
+            const int tm = tile / tiles_n, n0 = (tile - tm * tiles_n) * BN + c0;
+            const long long grow = (long long)tm * kTileRows + row;
+            const bool in_range = tile < total_tiles && grow < total_rows;
+            const int r = in_range ? (int)((unsigned)grow % (unsigned)p.M) : 0;
+            tok = in_range && p.idx ? __ldcg(p.idx + grow) : r;
+            before = in_range && p.idx && r > 0 ? __ldcg(p.idx + grow - 1) : -1;
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) xs_next[u] = in_range && u < k_steps ? __ldcg(p.x_scale + (long long)u * total_rows + grow) : 0.f;
+            ws_lane = tile < total_tiles && lane < k_steps ? __ldcg(p.w_scale + (long long)(n0 < p.N_out ? n0 / 128 : 0) * k_steps + lane) : 0.f;
+        };
+        fetch(pair);
         for (int tile = pair; tile < total_tiles; tile += n_pairs) {
             const int tm = tile / tiles_n, tn = tile - tm * tiles_n, n0 = tn * BN + c0;
             const long long grow = (long long)tm * kTileRows + row;
-            int batch = 0;
-            bool bad;
-            long long full_row = target_row(p, grow, total_rows, &batch, &bad);
+            const bool in_range = grow < total_rows;
+            // the row of a [B, N, *] tensor; -1: past the end, an entry out of range or one that does not exceed its predecessor
+            const int batch = in_range ? (int)((unsigned)grow / (unsigned)p.M) : 0;
+            const bool bad = in_range && ((unsigned)tok >= (unsigned)p.N || before >= tok);
+            const long long full_row = in_range && !bad ? (long long)batch * p.N + tok : -1;
             if (bad && tn == 0 && part == 0) atomicExch(p.err_word, kErrBadIndex);
-            const unsigned in_list = __ballot_sync(0xffffffffu, full_row >= 0);
-            const int batch0 = __shfl_sync(0xffffffffu, batch, in_list ? __ffs(in_list) - 1 : 0);
-            const bool one_batch = __all_sync(0xffffffffu, full_row < 0 || batch == batch0);       // (a gate belongs to a batch element)
-            // fetched while the blocks are summed: 8 columns of the bias (lanes 0-7) and of the gate (8-15), the first columns of the residual
-            uint4 vec = make_uint4(0, 0, 0, 0);
-            {
-                const int col = n0 + (lane & 7) * 8;
-                const __nv_bfloat16 *src = lane < 8 ? p.bias : EPI == kAnything && lane < 16 && p.gate ? p.gate + (long long)batch0 * p.N_out : nullptr;
-                if (src && (lane & 7) * 8 < kCols && col < p.N_out) vec = ld_cached(reinterpret_cast<const uint4 *>(src + col));
-            }
-            const long long res_row = (full_row >= 0 && p.res_compact) ? grow : full_row;
+            // the first columns of the residual are fetched while the blocks are summed
+            uint4 rr[kPieces];
+            auto residual_at = [&](int j, int col) -> const __nv_bfloat16 * {
+                const int rrow = __shfl_sync(0xffffffffu, full_row < 0 ? -1 : p.res_compact ? (int)grow : (int)full_row, r0 + kStep * j);
+                return rrow >= 0 && col < p.N_out ? p.residual + (long long)rrow * p.N_out + col : nullptr;
+            };
             if (EPI == kAnything && p.residual) {
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j) {
-                    const int r = r0 + kStep * j;
-                    const long long rrow = __shfl_sync(0xffffffffu, res_row, r);
-                    const bool there = rrow >= 0 && n0 + q * 8 < p.N_out;
-                    cp_async_16(s_stage + swizzled(r, q), p.residual + (there ? rrow * p.N_out + n0 + q * 8 : 0), there);
+                    const __nv_bfloat16 *src = residual_at(j, n0 + q * 8);
+                    cp_async_16(s_stage + swizzled(r0 + kStep * j, q), src ? src : p.residual, src != nullptr);
                 }
             }
-            const bool in_range = grow < total_rows;
-            const float *xs = p.x_scale + (in_range ? grow : 0);
-            const float *ws = p.w_scale + (long long)(n0 < p.N_out ? n0 / 128 : 0) * k_steps;
-            float xs_next = in_range ? __ldcg(xs) : 0.f, ws_lane = 0.f;
+            const float *xs = p.x_scale + (in_range ? grow : 0), *ws = p.w_scale + (long long)(n0 < p.N_out ? n0 / 128 : 0) * k_steps;
             f32x2 sum[kCols / 2];
 #pragma unroll
             for (int i = 0; i < kCols / 2; ++i) sum[i] = 0ull;
-            for (int ks = 0; ks < k_steps; ++ks, ++g) {
-                if ((ks & 31) == 0) ws_lane = ks + lane < k_steps ? __ldcg(ws + ks + lane) : 0.f;
-                const float s = xs_next * __shfl_sync(0xffffffffu, ws_lane, ks & 31);
-                if (ks + 1 < k_steps && in_range) xs_next = __ldcg(xs + (long long)(ks + 1) * total_rows);
-                const int acc = g % kAcc;
-                wait_bar(bar_acc_full + 8 * acc, (g / kAcc) & 1, &abort_flag, p.err_word);
-                tc_fence_after();
-                const f32x2 s2 = pack2(s, s);
+            for (int ks0 = 0; ks0 < k_steps; ks0 += kAhead) {
+                if (ks0 > 0 && (ks0 & 31) == 0) ws_lane = ks0 + lane < k_steps ? __ldcg(ws + ks0 + lane) : 0.f;
 #pragma unroll
-                for (int c = 0; c < kChunks; ++c) {
-                    uint32_t v[kChunk];
-                    tmem_ld<kChunk>(t_row + acc * BN + c * kChunk, v);
-                    tc_wait_ld();
-                    if (c == kChunks - 1) {                            // this warp's part of the accumulator has been read
+                for (int u = 0; u < kAhead; ++u) {
+                    const int ks = ks0 + u;
+                    if (ks >= k_steps) break;
+                    const float s1 = xs_next[u] * __shfl_sync(0xffffffffu, ws_lane, ks & 31);
+                    const f32x2 s = pack2(s1, s1);
+                    if (in_range && ks + kAhead < k_steps) xs_next[u] = __ldcg(xs + (long long)(ks + kAhead) * total_rows);
+                    wait_bar(bar_acc_full + 8 * acc, acc_phase, &abort_flag, p.err_word);
+                    tc_fence_after();
+                    const uint32_t t = t_row + acc * BN;
+                    auto release = [&] {                               // this warp's part of the accumulator has been read
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive_cluster(map_to_rank(bar_acc_empty + 8 * acc, 0));
-                    }
+                    };
 #pragma unroll
-                    for (int i = 0; i < kChunk / 2; ++i)
-                        sum[c * (kChunk / 2) + i] = fma2(pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), s2, sum[c * (kChunk / 2) + i]);
+                    for (int c = 0; c < kCols; c += kLoad) {
+                        f32x2 v[kLoad / 2];
+                        load_pairs<kLoad>(t + c, v);
+                        if (c + kLoad == kCols) release();
+#pragma unroll
+                        for (int i = 0; i < kLoad / 2; ++i) sum[c / 2 + i] = fma2(v[i], s, sum[c / 2 + i]);
+                    }
+                    if (++acc == kAcc) { acc = 0; acc_phase ^= 1; }
                 }
             }
             if (tile + n_pairs >= total_tiles) grid_launch_dependents();       // the last epilogue of this CTA
-            if (abort_flag) full_row = -1;
-            const long long out_row = (full_row >= 0 && p.compact) ? grow : full_row;
-            uint4 rr[kPieces];                                          // the residual of the next columns
+            fetch(tile + n_pairs);
+            int out_row[kPieces];                                           // rows r0 + kStep j of y
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j)
+                out_row[j] = __shfl_sync(0xffffffffu, full_row < 0 || abort_flag ? -1 : p.compact ? (int)grow : (int)full_row, r0 + kStep * j);
+            const __nv_bfloat16 *gate = p.gate ? p.gate + (long long)batch * p.N_out : nullptr;
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
-                const int colq = n0 + c * kChunk + q * 8;               // the 8 columns this lane moves
+                const int col0 = n0 + c * kChunk, colq = col0 + q * 8;      // this chunk's columns, the 8 that this lane moves
                 if (EPI == kAnything && p.residual) {
                     if (c == 0) asm volatile("cp.async.wait_all;" ::: "memory");
                     else {
@@ -208,45 +266,60 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                     if (c + 1 < kChunks) {
 #pragma unroll
                         for (int j = 0; j < kPieces; ++j) {
-                            const long long rrow = __shfl_sync(0xffffffffu, res_row, r0 + kStep * j);
-                            rr[j] = (rrow >= 0 && colq + kChunk < p.N_out) ? __ldcg(reinterpret_cast<const uint4 *>(p.residual + rrow * p.N_out + colq + kChunk))
-                                                                           : make_uint4(0, 0, 0, 0);
+                            const __nv_bfloat16 *src = residual_at(j, colq + kChunk);
+                            rr[j] = src ? __ldcg(reinterpret_cast<const uint4 *>(src)) : make_uint4(0, 0, 0, 0);
                         }
+                    }
+                }
+                // (all of a step's loads first, then its arithmetic: there are two warps on a scheduler to hide latencies)
+                f32x2 f[kChunk / 2];
+                uint4 vec[kPieces];
+                auto fetch_vector = [&](const __nv_bfloat16 *src) {
+#pragma unroll
+                    for (int v = 0; v < kPieces; ++v)
+                        vec[v] = col0 + v * 8 < p.N_out ? ld_cached(reinterpret_cast<const uint4 *>(src + col0 + v * 8)) : make_uint4(0, 0, 0, 0);
+                };
+                if (p.bias) {
+                    fetch_vector(p.bias);
+#pragma unroll
+                    for (int v = 0; v < kPieces; ++v) {
+                        f32x2 t[4];
+                        unpack8(vec[v], t);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) f[v * 4 + i] = add2(sum[c * 16 + v * 4 + i], t[i]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < kChunk / 2; ++i) f[i] = sum[c * 16 + i];
+                }
+                if (EPI == kGelu || (EPI == kAnything && p.gelu)) {
+#pragma unroll
+                    for (int i = 0; i < kChunk / 2; ++i) f[i] = gelu2_one_reciprocal(f[i]);
+                }
+                if (EPI == kAnything && gate) {
+                    fetch_vector(gate);
+#pragma unroll
+                    for (int v = 0; v < kPieces; ++v) {
+                        f32x2 t[4];
+                        unpack8(vec[v], t);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) f[v * 4 + i] = mul2(f[v * 4 + i], t[i]);
                     }
                 }
 #pragma unroll
                 for (int v = 0; v < kPieces; ++v) {
-                    const int col = n0 + c * kChunk + v * 8;
                     uint4 *mine = reinterpret_cast<uint4 *>(stage + swizzled(lane, v));     // residual in, result out
-                    f32x2 f[4], t[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) f[i] = sum[c * (kChunk / 2) + v * 4 + i];
-                    if (p.bias) {
-                        unpack8(shfl_vec(vec, c * kPieces + v), t);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) f[i] = add2(f[i], t[i]);
-                    }
-                    if (EPI == kGelu || (EPI == kAnything && p.gelu)) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) f[i] = gelu2(f[i]);
-                    }
-                    if (EPI == kAnything && p.gate) {
-                        uint4 gv = shfl_vec(vec, 8 + c * kPieces + v);
-                        if (!one_batch && col < p.N_out) gv = ld_cached(reinterpret_cast<const uint4 *>(p.gate + (long long)batch * p.N_out + col));
-                        unpack8(gv, t);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) f[i] = mul2(f[i], t[i]);
-                    }
                     if (EPI == kAnything && p.residual) {
+                        f32x2 t[4];
                         unpack8(*mine, t);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) f[i] = add2(f[i], t[i]);
+                        for (int i = 0; i < 4; ++i) f[v * 4 + i] = add2(f[v * 4 + i], t[i]);
                     }
                     uint32_t w[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         float lo, hi;
-                        unpack2(f[i], lo, hi);
+                        unpack2(f[v * 4 + i], lo, hi);
                         __nv_bfloat162 v2 = __floats2bfloat162_rn(lo, hi);
                         w[i] = *reinterpret_cast<uint32_t *>(&v2);
                     }
@@ -255,10 +328,8 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                 __syncwarp();
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j) {
-                    const int r = r0 + kStep * j;
-                    const long long orow = __shfl_sync(0xffffffffu, out_row, r);
-                    const uint4 t = *reinterpret_cast<const uint4 *>(stage + swizzled(r, q));
-                    if (orow >= 0 && colq < p.N_out) *reinterpret_cast<uint4 *>(p.y + orow * p.N_out + colq) = t;
+                    const uint4 t = *reinterpret_cast<const uint4 *>(stage + swizzled(r0 + kStep * j, q));
+                    if (out_row[j] >= 0 && colq < p.N_out) *reinterpret_cast<uint4 *>(p.y + (long long)out_row[j] * p.N_out + colq) = t;
                 }
                 __syncwarp();
             }
@@ -272,18 +343,19 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
             if (gave_up()) stop = min(stop, g);
             return stop > g;
         };
-        int g = 0;
+        int g = 0, st = 0;
+        uint32_t phase = 1;
         for (int tile = pair; tile < total_tiles; tile += n_pairs) {
             const int tm = tile / tiles_n, tn = tile - tm * tiles_n;
             for (int ks = 0; ks < k_steps; ++ks, ++g) {
-                const int st = g % kStages;
-                wait_bar(bar_empty + 8 * st, ((g / kStages) & 1) ^ 1, &abort_flag, p.err_word);
+                wait_bar(bar_empty + 8 * st, phase, &abort_flag, p.err_word);
                 if (elect_one() && going(g)) {
                     if (rank == 0) mbar_arrive_expect_tx(bar_full + 8 * st, 2 * (BN / 2 * kBK + kABytes));
                     tma_load_2d(sB + st * kBBytes, &tmap_w, full0 + 8 * st, ks * kBK, tn * BN + (int)rank * (BN / 2));
                     tma_load_2d(sA + st * kABytes, &tmap_x, full0 + 8 * st, ks * kBK, tm * kTileRows + (int)rank * kRowsCta);
                 }
                 __syncwarp();
+                if (++st == kStages) { st = 0; phase ^= 1; }
             }
         }
         // every copy issued above must have landed before either CTA's shared memory is released (see linear.cu)
@@ -295,23 +367,25 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         if (warp == kMmaWarp && rank == 0) {
             // -------------------------------------------- MMA issuer of the pair
             constexpr uint32_t idesc = idesc_e4m3(kTileRows, BN);
-            int g = 0;
+            const uint64_t desc_a = smem_desc(sA, 16, 1024, kSwizzle128B), desc_b = smem_desc(sB, 16, 1024, kSwizzle128B);    // of the first stage
+            int st = 0, acc = 0;
+            uint32_t phase = 0, acc_phase = 1;
             for (int tile = pair; tile < total_tiles; tile += n_pairs) {
-                for (int ks = 0; ks < k_steps; ++ks, ++g) {
-                    const int st = g % kStages, acc = g % kAcc;
-                    wait_bar<true>(bar_acc_empty + 8 * acc, ((g / kAcc) & 1) ^ 1, &abort_flag, p.err_word);
-                    wait_bar(bar_full + 8 * st, (g / kStages) & 1, &abort_flag, p.err_word);
-                    fence_acquire_smem();                              // what landed in the odd CTA is in order before the MMAs too
+                for (int ks = 0; ks < k_steps; ++ks) {
+                    // (what TMA has brought to either CTA is there for the MMAs once its bytes are counted: no fence between)
+                    wait_bar(bar_full + 8 * st, phase, &abort_flag, p.err_word);
+                    wait_bar<true>(bar_acc_empty + 8 * acc, acc_phase, &abort_flag, p.err_word);
                     tc_fence_after();
                     if (elect_one()) {
+                        const uint64_t a = desc_a + (uint32_t)st * (kABytes / 16), b = desc_b + (uint32_t)st * (kBBytes / 16);
 #pragma unroll
-                        for (int kk = 0; kk < kBK / 32; ++kk)
-                            mma_ss_pair_f8(tmem + acc * BN, smem_desc(sA + st * kABytes + kk * 32, 16, 1024, kSwizzle128B),
-                                           smem_desc(sB + st * kBBytes + kk * 32, 16, 1024, kSwizzle128B), idesc, kk > 0 ? 1u : 0u);
+                        for (int kk = 0; kk < kBK / 32; ++kk) mma_ss_pair_f8(tmem + acc * BN, a + kk * 2, b + kk * 2, idesc, kk > 0 ? 1u : 0u);
                         tc_commit_pair(bar_acc_full + 8 * acc);
                         tc_commit_pair(bar_empty + 8 * st);
                     }
                     __syncwarp();
+                    if (++st == kStages) { st = 0; phase ^= 1; }
+                    if (++acc == kAcc) { acc = 0; acc_phase ^= 1; }
                 }
             }
         }

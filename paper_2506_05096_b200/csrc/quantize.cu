@@ -16,34 +16,40 @@ constexpr float kE4M3Max = 448.0f, kLeastAmax = 7.888609052210118e-31f;       //
 constexpr int kWarps = 8;
 constexpr int kUnroll = 4;
 
-__device__ __forceinline__ uint32_t amax_bits(const uint4 &v) {               // largest magnitude of eight bf16, NaN left out
-    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-    __nv_bfloat162 m = __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[0]));
-#pragma unroll
-    for (int i = 1; i < 4; ++i) m = __hmax2(m, __habs2(*reinterpret_cast<const __nv_bfloat162 *>(&w[i])));
-    const __nv_bfloat16 s = __hmax(m.x, m.y);
-    return (uint32_t)*reinterpret_cast<const uint16_t *>(&s);
+// the larger magnitude of each half, NaN left out (signs are of no account until the end)
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+    uint32_t m;
+    asm("max.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(a), "r"(b));
+    return m;
 }
-__device__ __forceinline__ float as_float(uint32_t bf16_bits) { return __uint_as_float(bf16_bits << 16); }
+__device__ __forceinline__ uint32_t largest(const uint4 &v) { return larger(larger(v.x, v.y), larger(v.z, v.w)); }
+// of both halves, as fp32
+__device__ __forceinline__ float magnitude(uint32_t m) { return fmaxf(fabsf(__uint_as_float(m << 16)), fabsf(__uint_as_float(m & 0xffff0000u))); }
 
-struct BlockScale { float scale, inv; };
+// Quotients by the reciprocal and one residual step: q = a r, q + (a - q b) r.
+struct BlockScale { float scale, inv, minus; };
 __device__ __forceinline__ BlockScale scale_of(float amax) {
     BlockScale s;
-    s.scale = __fdiv_rn(fmaxf(amax, kLeastAmax), kE4M3Max);
-    s.inv = __frcp_rn(s.scale);
+    const float a = fmaxf(amax, kLeastAmax), q = a * (1.0f / kE4M3Max);
+    s.scale = fmaf(fmaf(q, -kE4M3Max, a), 1.0f / kE4M3Max, q);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s.scale));
+    s.inv = fmaf(fmaf(-s.scale, r, 1.0f), r, r);
+    s.minus = -s.scale;
+    // an infinity in the block: 0 for what is finite, NaN for what is not, and no residual
+    if (a == INFINITY) { s.scale = a; s.inv = 0.f; s.minus = 0.f; }
     return s;
 }
 // eight values as e4m3
 __device__ __forceinline__ uint2 encode8(const uint4 &v, const BlockScale &s) {
     f32x2 x[4];
     unpack8(v, x);
-    const f32x2 inv = pack2(s.inv, s.inv), minus = pack2(-s.scale, -s.scale);
+    const f32x2 inv = pack2(s.inv, s.inv), minus = pack2(s.minus, s.minus);
     uint32_t out[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         f32x2 q = mul2(x[i], inv);
-        // (an infinite scale: 0 for what is finite, NaN for what is not, and no residual)
-        if (s.inv != 0.f) q = fma2(fma2(q, minus, x[i]), inv, q);
+        q = fma2(fma2(q, minus, x[i]), inv, q);
         float lo, hi;
         unpack2(q, lo, hi);
         uint16_t c;
@@ -90,10 +96,10 @@ quantize_rows_kernel(const uint4 *__restrict__ x, const int32_t *__restrict__ id
 #pragma unroll
             for (int i = 0; i < kUnroll; ++i) {
                 const int c = (kb + 2 * i) * 16 + lane;
-                float m = as_float(amax_bits(v[i]));
+                uint32_t m = largest(v[i]);
 #pragma unroll
-                for (int o = 8; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-                const BlockScale s = scale_of(m);
+                for (int o = 8; o > 0; o >>= 1) m = larger(m, __shfl_xor_sync(0xffffffffu, m, o));
+                const BlockScale s = scale_of(magnitude(m));
                 if (c < k1 * 16) {
                     dst[c] = encode8(v[i], s);
                     if ((lane & 15) == 0) scale[(long long)(c >> 4) * rows + t] = s.scale;
@@ -117,7 +123,7 @@ quantize_weight_kernel(const uint4 *__restrict__ w, uint2 *__restrict__ wq, floa
     for (int i = 0; i < 8; ++i) {
         const int row = nb * 128 + r0 + 16 * i;
         v[i] = row < N_out ? ld_stream(w + ((long long)row * blocks + kb) * 16 + c) : make_uint4(0, 0, 0, 0);
-        m = fmaxf(m, as_float(amax_bits(v[i])));
+        m = fmaxf(m, magnitude(largest(v[i])));
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));

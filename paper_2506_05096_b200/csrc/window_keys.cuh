@@ -15,6 +15,8 @@ struct KeyList {
     int a1, b0, b1, c0, c1;              // ranges [0, a1), [b0, b1), [c0, c1), empty ones with no tile
     int b_tile, c_tile, n;               // number of the first tile of the second and third, tiles in all
     int all_lo, all_hi;                  // keys in reach of every row of the CTA
+    int w_base, w_tile, w_end;           // the range that holds the windows: its first key, its first tile, its end (none: 0, 0, 0)
+    int l_base, l_tile, l_end;           // and the one that holds the last keys
     __device__ __forceinline__ int key(int j) const { return j < b_tile ? kKeyTile * j : j < c_tile ? b0 + kKeyTile * (j - b_tile) : c0 + kKeyTile * (j - c_tile); }
     __device__ __forceinline__ int end(int j) const { return j < b_tile ? a1 : j < c_tile ? b1 : c1; }
 };
@@ -50,15 +52,30 @@ __device__ __forceinline__ KeyList list_keys(const WindowParams &p, int b, int f
     k.b_tile = (k.a1 + kKeyTile - 1) / kKeyTile;
     k.c_tile = k.b_tile + (k.b1 - k.b0 + kKeyTile - 1) / kKeyTile;
     k.n = k.c_tile + (k.c1 - k.c0 + kKeyTile - 1) / kKeyTile;
+    const bool b_there = k.b0 < k.b1, c_there = k.c0 < k.c1;
+    k.w_base = b_there ? k.b0 : 0; k.w_tile = b_there ? k.b_tile : 0; k.w_end = b_there ? k.b1 : k.a1;
+    k.l_base = c_there ? k.c0 : k.w_base; k.l_tile = c_there ? k.c_tile : k.w_tile; k.l_end = c_there ? k.c1 : k.w_end;
     k.all_lo = last - p.left; k.all_hi = rows ? first + p.right : -1;
     return k;
 }
 
-// Whether rows that all reach keys lo .. hi see every key of the tile from k0 (of a range that ends at `end`).
-__device__ __forceinline__ bool sees_all(int k0, int end, int lo, int hi, int n_first, int last0)
+// The tiles of which rows that all reach keys lo .. hi see every key: up to three runs of tile numbers (a tile that is seen whole only
+// because two reasons meet in it is not among them).
+struct WholeTiles {
+    int first, w0, w_n, l0, l_n;         // tiles below `first`, w_n from w0 on, l_n from l0 on
+    __device__ __forceinline__ bool has(int j) const { return j < first || (unsigned)(j - w0) < (unsigned)w_n || (unsigned)(j - l0) < (unsigned)l_n; }
+};
+__device__ __forceinline__ WholeTiles whole_tiles(const KeyList &k, int lo, int hi, int n_first, int last0)
 {
-    const int k1 = k0 + kKeyTile;
-    return k1 <= end && (k1 <= n_first || k0 >= last0 || (k0 >= lo && k1 - 1 <= hi));
+    WholeTiles t;
+    t.first = min(n_first, k.a1) / kKeyTile;
+    auto run = [](int from, int to, int base, int tile, int &t0, int &n) {      // keys from .. to - 1 of a range
+        const int a = (max(from - base, 0) + kKeyTile - 1) / kKeyTile, b = max(to - base, 0) / kKeyTile;
+        t0 = tile + a; n = max(b - a, 0);
+    };
+    run(lo, hi < k.w_end ? hi + 1 : k.w_end, k.w_base, k.w_tile, t.w0, t.w_n);
+    run(last0, k.l_end, k.l_base, k.l_tile, t.l0, t.l_n);
+    return t;
 }
 // bits [a, b) of a word, both clipped to [0, 64]
 __device__ __forceinline__ uint64_t bits_between(int a, int b)
@@ -152,9 +169,10 @@ __device__ __forceinline__ bool clean_values(uint4 *v, int rows, int lane)
 template <class T, int DH>
 __device__ __noinline__ void spread_odd_values(const WindowParams &p, const KeyList &keys, int tile0, int n_tiles, int b, int kv_head, int tok, T *row)
 {
+    const WholeTiles whole = whole_tiles(keys, keys.all_lo, keys.all_hi, p.n_first, p.last0);
     for (int j = 0; j < n_tiles; ++j) {
+        if (whole.has(tile0 + j)) continue;
         const int k0 = keys.key(tile0 + j), end = keys.end(tile0 + j);
-        if (sees_all(k0, end, keys.all_lo, keys.all_hi, p.n_first, p.last0)) continue;
         const uint64_t visible = visible_bits(k0, end, tok - p.left, tok + p.right, p.n_first, p.last0);
         for (int i = 0; i < kKeyTile; ++i) {
             if (!(visible >> i & 1)) continue;

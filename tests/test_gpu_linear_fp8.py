@@ -114,7 +114,8 @@ def close(got, want, mass, K, factor=1.0):
 
 
 @pytest.mark.parametrize("B,N,M,K,N_out", [(1, 4, 1, 128, 8), (1, 300, 77, 384, 200), (2, 150, 130, 1152, 264), (1, 600, 513, 256, 520),
-                                           (3, 40, 33, 2432, 64), (1, 256, 256, 128, 256), (1, 20000, 19000, 256, 1000), (2, 3000, 2999, 512, 2056)])
+                                           (3, 40, 33, 2432, 64), (1, 256, 256, 128, 256), (1, 20000, 19000, 256, 1000), (2, 3000, 2999, 512, 2056),
+                                           (1, 9000, 8200, 3200, 1032), (1, 9000, 8999, 128, 2048), (1, 5000, 4999, 1408, 2056)])
 def test_layer(B, N, M, K, N_out):
     g = torch.Generator("cuda").manual_seed(N_out + K)
     xq, xs, wq, ws = operands(g, B * M, N_out, K)

@@ -35,6 +35,7 @@ int main()
     std::mt19937 rng(1);
     auto upto = [&](int n) { return (int)(rng() % (unsigned)(n + 1)); };
     int n_case = 0;
+    long long runs = 0, missed = 0;                                // tiles seen whole that are in the runs, and that are not
     for (; n_case < 20000; ++n_case) {
         WindowParams p = {};
         p.N = p.N_tok = 1 + upto(n_case % 3 ? 700 : 60);
@@ -50,15 +51,17 @@ int main()
         for (int &r : rows) r = upto(p.N - 1);
         const int first = *std::min_element(rows.begin(), rows.end()), last = *std::max_element(rows.begin(), rows.end());
         const KeyList k = list_keys(p, 0, first, last);
-        int most = 0;
+        const WholeTiles whole = whole_tiles(k, k.all_lo, k.all_hi, p.n_first, p.last0);
         for (int r : rows) {
             std::vector<int> seen(p.N, 0);
+            const WholeTiles own = whole_tiles(k, r - p.left, r + p.right, p.n_first, p.last0);
             for (int j = 0; j < k.n; ++j) {
                 const int k0 = k.key(j), end = k.end(j);
                 CHECK(k0 >= 0 && k0 < end && end <= L);
                 const uint64_t bits = visible_bits(k0, end, r - p.left, r + p.right, p.n_first, p.last0);
-                if (sees_all(k0, end, k.all_lo, k.all_hi, p.n_first, p.last0)) CHECK(bits == ~0ull);
-                if (sees_all(k0, end, r - p.left, r + p.right, p.n_first, p.last0)) CHECK(bits == ~0ull);
+                if (whole.has(j)) CHECK(bits == ~0ull);
+                if (own.has(j)) { CHECK(bits == ~0ull); ++runs; }
+                if (bits == ~0ull && !own.has(j)) ++missed;
                 for (int i = 0; i < 64; ++i) if (bits >> i & 1) ++seen[k0 + i];
             }
             for (int j = 0; j < p.N; ++j) {
@@ -66,7 +69,6 @@ int main()
                 CHECK(seen[j] == (want ? 1 : 0));
             }
         }
-        (void)most;
         // no more tiles than the three ranges need
         const int a = min(p.n_first, L), b0 = min(max(first - p.left, 0), L), b1 = max(b0, min(last + p.right + 1, L)), c0 = min(p.last0, L);
         CHECK(k.n <= (a + 63) / 64 + (b1 - b0 + 63) / 64 + (L - c0 + 63) / 64);
@@ -76,6 +78,7 @@ int main()
         hide<64>(s, v, -1.f);
         for (int i = 0; i < 64; ++i) CHECK(s[i] == ((v >> i & 1) ? (float)i : -1.f));
     }
+    CHECK(runs > 100000 && missed * 20 < runs);
     WindowParams p = {};
     p.N = 100; p.last0 = 90; p.n_first = 5; p.left = p.right = 3;
     CHECK(list_keys(p, 0, 0x7fffffff, -1).n == 0);                // a unit whose rows are all bad entries
