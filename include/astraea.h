@@ -239,7 +239,7 @@ int32_t astraea_sparse_cross_attn(const void *q, const void *k, const void *v,
  *             stream's newest token against its cache: M = 1, q_idx its place, COMPACT_Q | COMPACT_OUT)
  *   k, v    : bf16 [B, N, H_kv, d] through their strides; keys that a row does not see, those from kv_len[b] on in
  *             particular, may hold anything, NaN included
- *   q_idx, M, out, lse_out, scale, flags : as astraea_sparse_attn (no SMALL_CTAS); N at most 2^30
+ *   q_idx, M, out, lse_out, scale, flags : as astraea_sparse_attn; N at most 2^30
  *   kv_len  : int32 [B] keys that exist (values outside [0, N] count as the nearer end); NULL => N
  *   workspace : 256-byte aligned, at least 256 bytes; with astraea_workspace_bytes(ASTRAEA_OP_WINDOW_ATTN, B, H, N, M, d) the
  *             units of a last, partial round (all units of a small call) may be shared out by keys over 2..16 CTAs each.  A

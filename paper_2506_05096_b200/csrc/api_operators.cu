@@ -21,11 +21,11 @@ int32_t astraea_window_attn(const void *q, const void *k, const void *v,
     const char *fn = "astraea_window_attn";
     REQUIRE(B > 0 && H > 0 && H_kv > 0 && N > 0, "%s: B, H, H_kv, N must be positive", fn);
     REQUIRE(N <= 1 << 30, "%s: N=%d is above 2^30", fn, N);
-    REQUIRE(H % H_kv == 0, "%s: H=%d must be a multiple of H_kv=%d", fn, H, H_kv);
+    REQUIRE(H % H_kv == 0 && H / H_kv <= 4096, "%s: H=%d must be a multiple of H_kv=%d, up to 4096 times it", fn, H, H_kv);
     REQUIRE(M >= 0 && M <= N, "%s: M=%d outside [0, N=%d]", fn, M, N);
     REQUIRE((long long)M * (H / H_kv) <= 1 << 30, "%s: too many rows", fn);
     if (d != 64 && d != 72 && d != 128) return fail(ASTRAEA_ERR_UNSUPPORTED, "%s: head_dim %d not in {64, 72, 128}", fn, d);
-    if (flags & ~(ASTRAEA_ATTN_COMPACT_OUT | ASTRAEA_ATTN_COMPACT_Q | ASTRAEA_ATTN_WHOLE_KEYS)) return fail(ASTRAEA_ERR_UNSUPPORTED, "%s: unknown flags 0x%x", fn, flags);
+    if (flags & ~(ASTRAEA_ATTN_COMPACT_OUT | ASTRAEA_ATTN_COMPACT_Q | ASTRAEA_ATTN_SMALL_CTAS | ASTRAEA_ATTN_WHOLE_KEYS)) return fail(ASTRAEA_ERR_UNSUPPORTED, "%s: unknown flags 0x%x", fn, flags);
     REQUIRE(n_first >= 0 && n_last >= 0 && left >= 0 && right >= 0, "%s: n_first, n_last, left, right must not be negative", fn);
     REQUIRE(q && k && v && out, "%s: null q, k, v or out", fn);
     REQUIRE(aligned16(q) && aligned16(k) && aligned16(v) && aligned16(out), "%s: q, k, v, out must be 16-byte aligned", fn);

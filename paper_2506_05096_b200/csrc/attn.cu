@@ -80,7 +80,6 @@ constexpr uint32_t kGaveUpLse = 0xffc0dead;
 // WIN: attention over a window of keys (window_keys.cuh).
 template <int DH, int TM, bool WIN = false> struct Cfg {
     static constexpr bool kWindow = WIN;
-    static_assert(!WIN || TM == 2, "windows: two query tiles per CTA");
     static_assert(TM == 2 || DH != 128, "head_dim 128 needs the whole SM");
     static constexpr int kDH = DH;
     static constexpr int kTilesM = TM;
@@ -91,7 +90,7 @@ template <int DH, int TM, bool WIN = false> struct Cfg {
     // rows are fetched.  Mostly launches over a few key tiles take this shape (cross-attention over the text tokens), where a unit
     // is 8 us of which 1-2 are its key loop: 9001 queries x 226 keys x 48 heads 92 -> 83 us.  (At head_dim 72 the same loop
     // spills and is 3 % slower; query rows fetched a unit ahead, in registers across the epilogue, spill: 103 us.)
-    static constexpr bool kPersistent = TM == 1 && DH == 64;
+    static constexpr bool kPersistent = TM == 1 && DH == 64 && !WIN;
     // head_dim = kMain (whole 64-column, 128-byte-swizzled chunks) + kTail (8 columns at head_dim 72,
     // carried as a 16-column, 32-byte-swizzled chunk whose upper half is zero)
     static constexpr int kMain = DH / 64 * 64;
@@ -442,22 +441,19 @@ __device__ __forceinline__ void pass_sync() {
     asm volatile("bar.sync 5, %0;" ::"n"(C::kThreads) : "memory");
 }
 
-// ---------------------------------------------------------------- softmax warpgroup
-// tile: its query tile; par: which key tiles it takes (j = par, par + kSplit, ...)
+// The Q rows of a query tile, by its two warpgroups (par 0 and 1).
 template <class C>
-__device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &bar, int tile, int par, uint8_t *sQ_gen, uint32_t tmem,
-                                             int m_base, int h, int b, int n_tiles, int key0, int part, bool last_unit,
-                                             volatile int *abort_flag, volatile int *redo_flag, float2 *xchg,
-                                             const KeyList *keys = nullptr, int tile0 = 0, volatile int *odd_flag = nullptr)
+__device__ __forceinline__ void gather_queries(const ParamsOf<C> &p, int par, uint8_t *sQ_gen, int m_base, int h, int b)
 {
     const int wtid = threadIdx.x & 127;
-    const int warp = __shfl_sync(0xffffffffu, wtid >> 5, 0);       // warp-uniform
     // gather this tile's Q rows (swizzled, K-major): 16-byte units, unit c of row r
     constexpr int kMainUnits = C::kMain / 8, kUnits = kMainUnits + (C::kTail ? 2 : 0);
     // (the warpgroups of a tile share the rows; all index loads first, then all row loads, then the stores, so that the
     // two dependent round trips to memory are paid once and not once per unit)
     constexpr int kGatherIters = kBlockM * kUnits / (128 * kSplit);
     static_assert(kBlockM * kUnits % (128 * kSplit) == 0, "whole iterations of the Q gather");
+    GroupRow first = {};                                   // the query and head of the tile's first row
+    if constexpr (C::kWindow) first = p.group_row(m_base);
     int gtok[kGatherIters];
 #pragma unroll
     for (int it = 0; it < kGatherIters; ++it) {
@@ -465,8 +461,9 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
         const int r = v / kUnits, c = v - r * kUnits;
         const int m = m_base + r;
         gtok[it] = -1;
-        if constexpr (C::kWindow) {                      // row m of the unit: query m / group of the list, head m % group of the key head
-            if (m < p.M * p.group && c * 8 < C::kDH) gtok[it] = p.q_compact ? m / p.group : p.token(b, m / p.group);
+        if constexpr (C::kWindow) {                      // row m of the launch: query m / group of the list, head m % group of the key head
+            const int query = first.m + p.div_group(first.rest + r);
+            if (query < p.M && c * 8 < C::kDH) gtok[it] = p.q_compact ? query : p.token(b, query);
         } else
         if (m < p.M && c * 8 < C::kDH)                   // the upper half of the tail chunk stays zero
             gtok[it] = p.q_idx ? __ldcg(p.q_idx + (size_t)b * p.M + m) : m;
@@ -479,7 +476,10 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
         gval[it] = make_uint4(0, 0, 0, 0);
         if ((unsigned)gtok[it] < (unsigned)p.N_tok) {
             int head = h;
-            if constexpr (C::kWindow) head = h * p.group + (m_base + v / kUnits) % p.group;
+            if constexpr (C::kWindow) {
+                const int x = first.rest + v / kUnits;
+                head = h * p.group + x - p.group * p.div_group(x);
+            }
             const __nv_bfloat16 *src = p.q + (size_t)b * p.q_sb + (size_t)gtok[it] * p.q_sn + (size_t)head * p.q_sh + c * 8;
             gval[it] = __ldcg(reinterpret_cast<const uint4 *>(src));
         }
@@ -493,6 +493,19 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
         else off = C::kChunks * C::kQChunkBytes + r * 32 + ((((c - kMainUnits) & 1) ^ ((r >> 2) & 1)) << 4);   // 32-byte swizzle
         *reinterpret_cast<uint4 *>(sQ_gen + off) = gval[it];
     }
+}
+
+// ---------------------------------------------------------------- softmax warpgroup
+// tile: its query tile; par: which key tiles it takes (j = par, par + kSplit, ...)
+template <class C>
+__device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &bar, int tile, int par, uint8_t *sQ_gen, uint32_t tmem,
+                                             int m_base, int h, int b, int n_tiles, int key0, int part, bool last_unit,
+                                             volatile int *abort_flag, volatile int *redo_flag, float2 *xchg,
+                                             const KeyList *keys = nullptr, int tile0 = 0, volatile int *odd_flag = nullptr)
+{
+    const int wtid = threadIdx.x & 127, kv_head = h;
+    const int warp = __shfl_sync(0xffffffffu, wtid >> 5, 0);       // warp-uniform
+    if constexpr (!C::kWindow) gather_queries<C>(p, par, sQ_gen, m_base, h, b);      // (windows: before the CTA's set-up was over)
     fence_proxy_async_smem();
     mbar_arrive(bar.q + 8 * tile);
 
@@ -509,9 +522,10 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
 
     int m = m_base + wtid;
     if constexpr (C::kWindow) {
-        const int g = m % p.group;
-        m /= p.group;
-        h = h * p.group + g;                                     // this row's head
+        const GroupRow at = p.group_row(m_base);
+        const int x = at.rest + wtid, more = p.div_group(x);
+        m = at.m + more;
+        h = h * p.group + x - p.group * more;                    // this row's head
     }
     int tok = -1;
     if (m < p.M) {
@@ -630,7 +644,7 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
     auto put_back = [&](auto *row) {
         if constexpr (C::kWindow) {
             const bool odd = pair_any(tile, *odd_flag != 0);     // (the row's two halves have been written; one answer for both warpgroups)
-            if (odd && par == 0 && row) spread_odd_values<std::remove_pointer_t<decltype(row)>, C::kDH>(p, *keys, tile0, n_tiles, b, h / p.group, tok, row);
+            if (odd && par == 0 && row) spread_odd_values<std::remove_pointer_t<decltype(row)>, C::kDH>(p, *keys, tile0, n_tiles, b, kv_head, tok, row);
         }
     };
     if (part >= 0) {
@@ -896,7 +910,8 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
         // tiles there are.  Entries that are not written (see softmax_role) do not count.
         if (warp == kProducerWarp) {
             grid_dependency_wait();
-            const int m_first = m0 / p.group, m_end = min(p.M, (m0 + kTilesM * kBlockM - 1) / p.group + 1);
+            const GroupRow at = p.group_row(m0);
+            const int m_first = at.m, m_end = min(p.M, at.m + p.div_group(at.rest + kTilesM * kBlockM - 1) + 1);
             int first = INT_MAX, last = -1;
             constexpr int kEntries = kTilesM * kBlockM / 32 + 1;
 #pragma unroll
@@ -926,6 +941,15 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     if (warp == kIssuerWarp) {
         tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
         tmem_relinquish();
+    }
+    if constexpr (C::kWindow) {
+        // The Q rows are two round trips to memory (list, rows): they run under the set-up, whose longest part is the list of key tiles.
+        // (Nothing reads them before the tile's barrier, which is arrived at behind the CTA-wide one.)
+        if (warp < C::kSoftmaxWarps && warp / (4 * kSplit) < q_tiles) {
+            const int tile = warp / (4 * kSplit);
+            grid_dependency_wait();
+            gather_queries<C>(p, warp / 4 % kSplit, smem_gen + tile * C::kQTileBytes, m0 + tile * kBlockM, h, b);
+        }
     }
     tc_fence_before();
     __syncthreads();
@@ -1510,7 +1534,7 @@ struct Schedule { bool small = false; SplitPlan plan; };
 double finish_time(long long units, int pairs, bool light_last, int n_sm, int tail_units, int split, double share_cost = 0.03)
 {
     // greedy dispatch in launch order: every CTA goes to the SM that is free first (a binary min-heap of busy times)
-    double heap[kMaxSMs] = {};
+    double heap[2 * kMaxSMs] = {};                               // (n_sm: slots for CTAs, two per SM for small ones)
     double finish = 0.0;
     auto put = [&](double cost) {
         const double t = heap[0] + cost;
@@ -1618,7 +1642,8 @@ __global__ void __launch_bounds__(ROWS) merge_window_kernel(const __grid_constan
     const int idx = blockIdx.x * ROWS + threadIdx.x;
     const int r = idx / kChunksRow, c = idx - r * kChunksRow;
     if (m0 + r >= p.M * p.group) return;
-    const int m = (m0 + r) / p.group, h = kv * p.group + (m0 + r) % p.group;
+    const GroupRow at = p.group_row(m0);
+    const int x = at.rest + r, more = p.div_group(x), m = at.m + more, h = kv * p.group + x - p.group * more;
     const int tok = p.token(b, m), before = (p.q_idx && m > 0) ? p.token(b, m - 1) : -1;
     const size_t part0 = (size_t)blockIdx.y * p.split;
     float lse[kMaxWindowSplit], mx = -INFINITY;
@@ -1667,52 +1692,53 @@ __global__ void __launch_bounds__(ROWS) merge_window_kernel(const __grid_constan
     }
 }
 
-// Key tiles that a unit has, as far as the host can tell: 256 rows of an evenly spread list and what is in reach of them.
-long long window_tiles(const WindowArgs &a)
+// Key tiles that a unit of `rows` rows has, as far as the host can tell: those of an evenly spread list and what is in reach of them.
+long long window_tiles(const WindowArgs &a, int unit_rows)
 {
-    const long long rows = a.a.M < 256 / a.group + 1 ? a.a.M : 256 / a.group + 1;
+    const long long rows = a.a.M < unit_rows / a.group + 1 ? a.a.M : unit_rows / a.group + 1;
     const long long span = a.a.M > 1 ? rows * a.a.N_tok / a.a.M : 1, keys = span + a.left + a.right + a.n_first + a.n_last;
     return ((keys < a.a.N ? keys : a.a.N) + kKeyTile - 1) / kKeyTile;
 }
 
 // The last, partial round of CTAs shares its units' key tiles where that finishes earlier.  A share costs about what four key tiles do on
 // top of its own (positions, query rows, the pipeline, its fp32 rows and their part in the merge).
-SplitPlan window_plan(const WindowArgs &a)
+SplitPlan window_plan(const WindowArgs &a, int tm)
 {
     SplitPlan plan;
+    const int unit_rows = tm * kBlockM, slots = sm_count() * (tm == 1 ? 2 : 1);
     const long long rows = (long long)a.a.M * a.group, hb = (long long)a.a.H / a.group * a.a.B;
-    const int pairs = (int)((rows + 2 * kBlockM - 1) / (2 * kBlockM)), n_sm = sm_count();
-    const long long units = hb * pairs;
-    const bool light_last = rows - (long long)(pairs - 1) * 2 * kBlockM <= kBlockM;
-    if (!a.a.split_ws || units > 16 * n_sm) return plan;
-    const long long tiles = window_tiles(a);
-    const int tail = (int)(units % n_sm);
+    const int groups = (int)((rows + unit_rows - 1) / unit_rows);
+    const long long units = hb * groups;
+    const bool light_last = tm == 2 && rows - (long long)(groups - 1) * unit_rows <= kBlockM;
+    if (!a.a.split_ws || units > 16 * slots) return plan;
+    const long long tiles = window_tiles(a, unit_rows);
+    const int tail = (int)(units % slots);
     if (tail == 0) return plan;
     // a stream's steps repeat a few shapes, and the estimate takes 20-150 us: the last answers are kept
-    struct Memo { long long units = -1, tiles = -1; int pairs = 0, n_sm = 0, d = 0; bool light_last = false; size_t ws = 0; SplitPlan plan; };
+    struct Memo { long long units = -1, tiles = -1; int groups = 0, slots = 0, d = 0; bool light_last = false; size_t ws = 0; SplitPlan plan; };
     constexpr int kMemo = 16;
     thread_local Memo memo[kMemo];
     thread_local int memo_next = 0;
     for (const Memo &e : memo)
-        if (e.units == units && e.tiles == tiles && e.pairs == pairs && e.light_last == light_last && e.n_sm == n_sm && e.d == a.a.d && e.ws == a.a.split_ws_bytes)
+        if (e.units == units && e.tiles == tiles && e.groups == groups && e.light_last == light_last && e.slots == slots && e.d == a.a.d && e.ws == a.a.split_ws_bytes)
             return e.plan;
-    const double whole = finish_time(units, pairs, light_last, n_sm, 0, 1);
+    const double whole = finish_time(units, groups, light_last, slots, 0, 1);
     double best = whole;
     for (int s = 2; s <= kMaxWindowSplit && s * 2 <= tiles; ++s) {
         if ((long long)tail * s > kMaxSplitParts || split_bytes((long long)tail * s, a.a.d) > a.a.split_ws_bytes) break;
-        const double t = finish_time(units, pairs, light_last, n_sm, tail, s, 4.0 / (double)tiles);
+        const double t = finish_time(units, groups, light_last, slots, tail, s, 4.0 / (double)tiles);
         if (t < 0.97 * whole && t < best) { best = t; plan.units = tail; plan.split = s; }
     }
     Memo &e = memo[memo_next];
     memo_next = (memo_next + 1) % kMemo;
-    e.units = units; e.tiles = tiles; e.pairs = pairs; e.light_last = light_last; e.n_sm = n_sm; e.d = a.a.d; e.ws = a.a.split_ws_bytes; e.plan = plan;
+    e.units = units; e.tiles = tiles; e.groups = groups; e.light_last = light_last; e.slots = slots; e.d = a.a.d; e.ws = a.a.split_ws_bytes; e.plan = plan;
     return plan;
 }
 
-template <int DH>
+template <int DH, int TM>
 int32_t launch_window_dh(const WindowArgs &w, cudaStream_t stream)
 {
-    using C = Cfg<DH, 2, true>;
+    using C = Cfg<DH, TM, true>;
     const AttnArgs &a = w.a;
     const int kv_heads = a.H / w.group;
     CUtensorMap mk, mv, mkt, mvt;
@@ -1741,37 +1767,42 @@ int32_t launch_window_dh(const WindowArgs &w, cudaStream_t stream)
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.compact = (a.flags & ASTRAEA_ATTN_COMPACT_OUT) ? 1 : 0;
     p.err_word = a.err_word;
-    p.tiles_x = (int)(((long long)a.M * w.group + 2 * kBlockM - 1) / (2 * kBlockM));
+    p.tiles_x = (int)(((long long)a.M * w.group + TM * kBlockM - 1) / (TM * kBlockM));
     p.heads = kv_heads;
-    p.group = w.group; p.left = w.left; p.right = w.right; p.n_first = w.n_first; p.last0 = a.N - w.n_last;
+    p.group = w.group; p.group_inv = ((1ull << 32) + w.group - 1) / w.group; p.left = w.left; p.right = w.right; p.n_first = w.n_first; p.last0 = a.N - w.n_last;
     p.kv_len = w.kv_len;
     p.q_compact = (a.flags & ASTRAEA_ATTN_COMPACT_Q) ? 1 : 0;
     p.v = reinterpret_cast<const __nv_bfloat16 *>(a.v);
     p.v_sb = a.v_sb; p.v_sh = a.v_sh; p.v_sn = a.v_sn;
     const long long units = (long long)p.tiles_x * kv_heads * a.B;
     if (units + kMaxSplitParts > 0x7fffffffll) return fail(ASTRAEA_ERR_INVALID_ARG, "astraea_window_attn: too many CTAs");
-    const SplitPlan plan = (a.flags & ASTRAEA_ATTN_WHOLE_KEYS) ? SplitPlan() : window_plan(w);
+    const SplitPlan plan = (a.flags & ASTRAEA_ATTN_WHOLE_KEYS) ? SplitPlan() : window_plan(w, TM);
     const bool split = plan.split > 1;
     p.n_full = (int)units - (split ? plan.units : 0);
     p.split = plan.split;
     if (split) {
-        const size_t rows = (size_t)plan.units * plan.split * (2 * kBlockM);
+        const size_t rows = (size_t)plan.units * plan.split * (TM * kBlockM);
         p.part_lse = reinterpret_cast<float *>(static_cast<char *>(a.split_ws));
         p.part_o = p.part_lse + (rows + 63) / 64 * 64;
     }
     p.n_ctas = p.n_full + (split ? plan.units * plan.split : 0);
     launch_overlapped(sparse_attn_kernel<C>, (unsigned)p.n_ctas, C::kThreads, C::kSmemBytes, stream, mk, mv, mkt, mvt, p);
-    if (split) launch_overlapped(merge_window_kernel<DH, 2 * kBlockM>, dim3(DH / 8, plan.units), 2 * kBlockM, 0, stream, p);
+    if (split) launch_overlapped(merge_window_kernel<DH, TM * kBlockM>, dim3(DH / 8, plan.units), TM * kBlockM, 0, stream, p);
     return check_launch("astraea_window_attn");
 }
 }  // namespace
 
 int32_t launch_window_attn(const WindowArgs &w, cudaStream_t stream)
 {
+    // Small CTAs (one query tile, two on an SM) overlap one's start and end, 6-9 us, with the other's key loop and see fewer keys that only
+    // other rows need; large ones have the faster loop.  us with large / small CTAs by key tiles of a unit of 256 rows: head_dim 72, 6553
+    // consecutive of 16384 x 32 heads, 4 tiles 77 / 57, 20 164 / 146, 63 379 / 349, 111 587 / 575, 90 tiles of a list 466 / 435; head_dim 64, 4613
+    // of 17776 x 24 heads, 4 34 / 25, 34 105 / 101, 60 163 / 169, 103 269 / 267; over all keys (256 tiles and more) the large ones win by 5 and 17 %.
+    const bool small = w.a.d != 128 && ((w.a.flags & ASTRAEA_ATTN_SMALL_CTAS) || window_tiles(w, 2 * kBlockM) <= (w.a.d == 72 ? 112 : 40));
     switch (w.a.d) {
-    case 64: return launch_window_dh<64>(w, stream);
-    case 72: return launch_window_dh<72>(w, stream);
-    case 128: return launch_window_dh<128>(w, stream);
+    case 64: return small ? launch_window_dh<64, 1>(w, stream) : launch_window_dh<64, 2>(w, stream);
+    case 72: return small ? launch_window_dh<72, 1>(w, stream) : launch_window_dh<72, 2>(w, stream);
+    case 128: return launch_window_dh<128, 2>(w, stream);
     default: return fail(ASTRAEA_ERR_UNSUPPORTED, "head_dim %d is not supported", w.a.d);
     }
 }

@@ -21,8 +21,13 @@ struct KeyList {
     __device__ __forceinline__ int end(int j) const { return j < b_tile ? a1 : j < c_tile ? b1 : c1; }
 };
 
+struct GroupRow { int m, rest; };        // row m * group + rest of a key head's (query, head) pairs
 struct WindowParams : Params {
     int group;                           // query heads of a key head: `heads` of the launch are key heads, a unit's rows are (query, head) pairs
+    uint64_t group_inv;                  // 2^32 / group, rounded up
+    // x / group for x below 256 + group, exact while that times the group is below 2^32 (the group is at most 4096)
+    __host__ __device__ __forceinline__ int div_group(int x) const { return (int)((uint32_t)x * group_inv >> 32); }
+    __device__ __forceinline__ GroupRow group_row(int row) const { const int m = row / group; return {m, row - m * group}; }
     int left, right, n_first, last0;     // last0 = N - n_last
     const int32_t *kv_len;               // keys of a batch element that exist (NULL: all N)
     int q_compact;                       // q holds the listed rows only

@@ -78,10 +78,11 @@ def run(g, B, N, M, H, H_kv, d, n_first=0, n_last=0, left=0, right=0, kv_len=Non
 @pytest.mark.parametrize("N,M,left,right,n_first,n_last", [
     (1, 1, 0, 0, 0, 0), (64, 64, 0, 0, 0, 0), (65, 65, 5, 3, 0, 0), (300, 140, 20, 0, 7, 0), (300, 140, 0, 40, 0, 9), (700, 700, 100, 100, 64, 64),
     (1000, 129, 63, 64, 1, 1), (1000, 257, 1000, 0, 0, 0), (1000, 31, 2000000000, 2000000000, 0, 0), (513, 300, 17, 17, 513, 0), (513, 300, 17, 17, 0, 513),
-    (2000, 600, 300, 300, 100, 77)])
-def test_windows(d, N, M, left, right, n_first, n_last):
+    (2000, 600, 300, 300, 100, 77), (9000, 500, 8000, 500, 0, 0)])
+@pytest.mark.parametrize("flags", [0, A.ATTN_SMALL_CTAS])
+def test_windows(d, N, M, left, right, n_first, n_last, flags):
     g = torch.Generator("cuda").manual_seed(N + d)
-    check(*run(g, 2, N, M, 3, 3, d, n_first, n_last, left, right))
+    check(*run(g, 2, N, M, 3, 3, d, n_first, n_last, left, right, flags=flags))
 
 
 @pytest.mark.parametrize("d", [64, 72, 128])

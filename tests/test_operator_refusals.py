@@ -83,7 +83,7 @@ def test_window_attention(L):
         return L.astraea_window_attn(q, k, v, *qs, *ks, *ks, idx, M, kv_len, out, None, B, H, H_kv, N, d, n_first, n_last, left, right, scale, flags,
                                      ws, size, None)
 
-    assert call(d=96) == A.ERR_UNSUPPORTED and call(flags=A.ATTN_SMALL_CTAS) == A.ERR_UNSUPPORTED and call(flags=16) == A.ERR_UNSUPPORTED
+    assert call(d=96) == A.ERR_UNSUPPORTED and call(flags=16) == A.ERR_UNSUPPORTED
     assert call(ws=None) == A.ERR_WORKSPACE_TOO_SMALL and call(size=255) == A.ERR_WORKSPACE_TOO_SMALL
     for bad in (dict(q=None), dict(k=None), dict(v=None), dict(out=None), dict(q=P + 8), dict(out=P + 8), dict(qs=(1024, 64, 100)), dict(ks=(1024, 60, 128)),
                 dict(qs=(1024, 64, 32)), dict(ks=(-8, 64, 128)), dict(M=17), dict(M=-1), dict(B=0), dict(H=3), dict(H_kv=0), dict(N=0), dict(N=(1 << 30) + 1),

@@ -13,6 +13,7 @@
 using std::max;
 using std::min;
 #define __device__
+#define __host__
 #define __forceinline__ inline
 #define __noinline__
 struct uint4 { uint32_t x, y, z, w; };
@@ -79,6 +80,12 @@ int main()
         for (int i = 0; i < 64; ++i) CHECK(s[i] == ((v >> i & 1) ? (float)i : -1.f));
     }
     CHECK(runs > 100000 && missed * 20 < runs);
+    for (int g = 1; g <= 4096; ++g) {                              // a row's query and head
+        WindowParams q = {};
+        q.group = g; q.group_inv = ((1ull << 32) + g - 1) / g;
+        for (int x = 0; x < g + 256; ++x) CHECK(q.div_group(x) == x / g);
+        CHECK(q.group_row((1 << 30) - 1).m == ((1 << 30) - 1) / g);
+    }
     WindowParams p = {};
     p.N = 100; p.last0 = 90; p.n_first = 5; p.left = p.right = 3;
     CHECK(list_keys(p, 0, 0x7fffffff, -1).n == 0);                // a unit whose rows are all bad entries
