@@ -134,6 +134,11 @@ int32_t launch_quantize_fp8_weight(const void *w, void *wq, float *w_scale, int 
 int32_t launch_gathered_linear_fp8(const void *xq, const float *x_scale, const int32_t *idx, int M, const void *wq, const float *w_scale,
                                    const void *bias, const void *residual, const void *gate, void *y, int B, int N, int K, int N_out,
                                    uint32_t flags, int *err_word, cudaStream_t stream);
+// the same for at most kFewRows rows
+constexpr int kFewRows = 8;
+int32_t launch_linear_fp8_rows(const void *xq, const float *x_scale, const int32_t *idx, int M, const void *wq, const float *w_scale,
+                               const void *bias, const void *residual, const void *gate, void *y, int B, int N, int K, int N_out,
+                               uint32_t flags, int *err_word, cudaStream_t stream);
 
 struct AttnArgs {
     const void *q, *k, *v;

@@ -450,6 +450,8 @@ int32_t launch_gathered_linear_fp8(const void *xq, const float *x_scale, const i
                                    const void *bias, const void *residual, const void *gate, void *y, int B, int N, int K, int N_out,
                                    uint32_t flags, int *err_word, cudaStream_t stream)
 {
+    if ((long long)B * (idx ? M : N) <= kFewRows)
+        return launch_linear_fp8_rows(xq, x_scale, idx, idx ? M : N, wq, w_scale, bias, residual, gate, y, B, N, K, N_out, flags, err_word, stream);
     Fp8Params p = {};
     p.x_scale = x_scale; p.w_scale = w_scale; p.idx = idx;
     p.M = idx ? M : N; p.B = B; p.N = N; p.K = K; p.N_out = N_out;
