@@ -42,7 +42,8 @@ constexpr int kMaxAcc = 4;
 constexpr int kAhead = 4;                                              // blocks between the load of a row's scale and its use
 constexpr int kBarBytes = 256;
 static_assert(8 * (2 * kStages + 2 * kMaxAcc + 1) <= kBarBytes, "barrier area too small");
-constexpr int kSmemBytes = kStages * (kABytes + kBBytes) + kBarBytes + kSumWarps * kStageBytes + 1024;
+constexpr int kVecBytes = 2 * 256;                                     // per sum warp: its columns of the bias and of a gate
+constexpr int kSmemBytes = kStages * (kABytes + kBBytes) + kBarBytes + kSumWarps * (kStageBytes + kVecBytes) + 1024;
 static_assert(kSmemBytes + 512 <= 227 * 1024, "shared memory of one CTA");
 constexpr uint32_t kTmemCols = 512;
 // registers: 128 sums, 64 values on their way out of TMEM and the addresses of a sum warp against 168 a thread at launch
@@ -169,6 +170,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + c0;
         uint8_t *stage = smem_raw + (bars + kBarBytes - smem_u32(smem_raw)) + warp * kStageBytes;
         const uint32_t s_stage = smem_u32(stage);
+        uint8_t *vectors = smem_raw + (bars + kBarBytes - smem_u32(smem_raw)) + kSumWarps * kStageBytes + warp * kVecBytes;
         // A thread owns a row of the tile, and global memory is touched in 16-byte pieces: piece q of rows r0 + kStep j (see linear.cu; a bulk
         // copy of each row's 64 bytes instead, by its own thread, took 1.4 times as long for 13106 x 1152 x 4608)
         constexpr int kPieces = kChunk / 8, kStep = 32 / kPieces;
@@ -179,6 +181,8 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         // What a tile needs before its first block: the list's entries for its rows, the scales of the first blocks.  They are fetched in
         // front of the epilogue of the tile before (behind it, they were 1500 clocks of every tile).
         int tok = 0, before = -1;
+        uint4 vec_next = make_uint4(0, 0, 0, 0);                       // lanes 0-15: 8 columns of the bias each, 16-31: of the gate
+        int vec_batch = -1;                                            // the batch element that the gate belongs to
         float xs_next[kAhead], ws_lane = 0.f;                          // scales of the row, kAhead blocks ahead (an L2 round trip is longer than a block)
         auto fetch = [&](int tile) {
             const int tm = tile / tiles_n, n0 = (tile - tm * tiles_n) * BN + c0;
@@ -190,6 +194,10 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) xs_next[u] = in_range && u < k_steps ? __ldcg(p.x_scale + (long long)u * total_rows + grow) : 0.f;
             ws_lane = tile < total_tiles && lane < k_steps ? __ldcg(p.w_scale + (long long)(n0 < p.N_out ? n0 / 128 : 0) * k_steps + lane) : 0.f;
+            vec_batch = __shfl_sync(0xffffffffu, in_range ? (int)((unsigned)grow / (unsigned)p.M) : 0, 0);
+            const __nv_bfloat16 *src = lane < 16 ? p.bias : EPI == kAnything && p.gate ? p.gate + (long long)vec_batch * p.N_out : nullptr;
+            const int col = n0 + (lane & 15) * 8;
+            vec_next = src && tile < total_tiles && (lane & 15) * 8 < kCols && col < p.N_out ? ld_cached(reinterpret_cast<const uint4 *>(src + col)) : make_uint4(0, 0, 0, 0);
         };
         fetch(pair);
         for (int tile = pair; tile < total_tiles; tile += n_pairs) {
@@ -201,6 +209,9 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
             const bool bad = in_range && ((unsigned)tok >= (unsigned)p.N || before >= tok);
             const long long full_row = in_range && !bad ? (long long)batch * p.N + tok : -1;
             if (bad && tn == 0 && part == 0) atomicExch(p.err_word, kErrBadIndex);
+            // the vectors go to shared memory, where every row's thread finds them (the last tile's have been used: the warp has met since)
+            *reinterpret_cast<uint4 *>(vectors + lane * 16) = vec_next;
+            const bool one_batch = __all_sync(0xffffffffu, full_row < 0 || batch == vec_batch);       // (a gate belongs to a batch element)
             // the first columns of the residual are fetched while the blocks are summed
             uint4 rr[kPieces];
             auto residual_at = [&](int j, int col) -> const __nv_bfloat16 * {
@@ -274,13 +285,9 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                 // (all of a step's loads first, then its arithmetic: there are two warps on a scheduler to hide latencies)
                 f32x2 f[kChunk / 2];
                 uint4 vec[kPieces];
-                auto fetch_vector = [&](const __nv_bfloat16 *src) {
-#pragma unroll
-                    for (int v = 0; v < kPieces; ++v)
-                        vec[v] = col0 + v * 8 < p.N_out ? ld_cached(reinterpret_cast<const uint4 *>(src + col0 + v * 8)) : make_uint4(0, 0, 0, 0);
-                };
                 if (p.bias) {
-                    fetch_vector(p.bias);
+#pragma unroll
+                    for (int v = 0; v < kPieces; ++v) vec[v] = *reinterpret_cast<const uint4 *>(vectors + (c * kPieces + v) * 16);
 #pragma unroll
                     for (int v = 0; v < kPieces; ++v) {
                         f32x2 t[4];
@@ -297,7 +304,10 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                     for (int i = 0; i < kChunk / 2; ++i) f[i] = gelu2_one_reciprocal(f[i]);
                 }
                 if (EPI == kAnything && gate) {
-                    fetch_vector(gate);
+#pragma unroll
+                    for (int v = 0; v < kPieces; ++v)
+                        vec[v] = one_batch ? *reinterpret_cast<const uint4 *>(vectors + 256 + (c * kPieces + v) * 16)
+                               : col0 + v * 8 < p.N_out ? ld_cached(reinterpret_cast<const uint4 *>(gate + col0 + v * 8)) : make_uint4(0, 0, 0, 0);
 #pragma unroll
                     for (int v = 0; v < kPieces; ++v) {
                         f32x2 t[4];
