@@ -5,11 +5,14 @@
 // (Section 3.2: such layers act on every token by itself, so queries are needed for the selected tokens only; keys for all).
 //
 // HBM-bound: every value is read once and written once, in one launch for queries and keys.  A warp takes one token's heads (a share of
-// them in short launches); what weights, cosines and sines make of a channel pair is two products and a sum, whose factors are computed
-// once per token and used for all of its heads.  A lane owns the same channels of the first and of the second half of a head (16 bytes
-// each; three times 8 bytes at head_dim 72, whose halves are 72 bytes), so that both ways of pairing channels, (2p, 2p + 1) and
-// (p, p + d/2), stay inside a lane and only the sums of the norm go round: over 4, 3 or 8 lanes.
+// them in short launches), whose cosines and sines it reads once.  A lane owns the same channels of the first and of the second half of a
+// head (16 bytes each; three times 8 bytes at head_dim 72, whose halves are 72 bytes), so that both ways of pairing channels, (2p, 2p + 1)
+// and (p, p + d/2), stay inside a lane and only the sums of the norm go round: over 4, 3 or 8 lanes.  The rows come through shared memory by
+// cp.async, one or two rounds of heads ahead, so that the loads of the next token run under the arithmetic of this one and cost no registers
+// (with loads into registers 71280 query and 118800 key rows of 24 x 128 took 412 us, now 385 = 6.2 TB/s).
 // fp32 arithmetic, one rounding to bf16 at the end.
+#include <initializer_list>
+
 #include "common.cuh"
 
 namespace astraea {
@@ -35,13 +38,25 @@ struct HeadNormParams {
     int *err_word;
 };
 
-template <int DH, bool LAYER = false> struct Lanes {
+template <int DH> struct Lanes {
     static constexpr int kUnit = DH == 72 ? 4 : 8;                 // channels of one access
     static constexpr int kUnits = DH == 72 ? 3 : 1;                // accesses of a lane to each half of a head
     static constexpr int kGroup = DH / 2 / (kUnit * kUnits);       // lanes of a head: 4, 3, 8
     static constexpr int kHeads = 32 / kGroup;                     // heads that a warp takes at once: 8, 10, 4
-    static constexpr int kUnroll = DH == 72 ? 2 : LAYER ? 3 : 6;              // and how often before it waits (24 x 128, 16 x 72, 48 x 64 are one round)
+    static constexpr int kUnroll = DH == 72 ? 2 : 6;              // and how often before it waits (24 x 128, 16 x 72, 48 x 64 are one round)
 };
+
+// What a warp keeps of a round in shared memory: kUnroll * kHeads heads as they lie in memory, and the cosines and sines of their token.
+// Two of them: the next round is on its way while one is worked on.
+template <int DH> struct Round {
+    using L = Lanes<DH>;
+    static constexpr int kHeadVecs = DH / 8, kHeads = L::kUnroll * L::kHeads, kVecs = kHeads * kHeadVecs;      // 16-byte pieces
+    static constexpr int kTableVecs = DH / 8;                      // of the cosines; as many of the sines
+    static constexpr int kBytes = (kVecs + 2 * kTableVecs) * 16;
+};
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 
 // one access to a head: 16 or 8 bytes
 template <int U> __device__ __forceinline__ void load_unit(const __nv_bfloat16 *p, uint32_t *r) {
@@ -62,17 +77,7 @@ template <int U> __device__ __forceinline__ void store_unit(__nv_bfloat16 *p, co
     if constexpr (U == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
 }
-// N consecutive values of a table
-template <int N> __device__ __forceinline__ void load_table(const float *p, float *f) {
-    if constexpr (N == 2) asm volatile("ld.global.v2.f32 {%0,%1}, [%2];" : "=f"(f[0]), "=f"(f[1]) : "l"(p));
-    else {
-#pragma unroll
-        for (int i = 0; i < N; i += 4)
-            asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f[i]), "=f"(f[i + 1]), "=f"(f[i + 2]), "=f"(f[i + 3]) : "l"(p + i));
-    }
-}
 __device__ __forceinline__ f32x2 widen(uint32_t w) { return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
-__device__ __forceinline__ f32x2 swapped(uint32_t w) { return pack2(__uint_as_float(w & 0xffff0000u), __uint_as_float(w << 16)); }
 __device__ __forceinline__ f32x2 swapped(f32x2 v) { float lo, hi; unpack2(v, lo, hi); return pack2(hi, lo); }
 __device__ __forceinline__ f32x2 twice(float v) { return pack2(v, v); }
 
@@ -92,119 +97,131 @@ template <int G> __device__ __forceinline__ float group_sum(float s, int lane) {
 template <int DH, bool LAYER, bool HALF>
 __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_norm_kernel(const __grid_constant__ HeadNormParams p)
 {
-    using L = Lanes<DH, LAYER>;
+    using L = Lanes<DH>;
     constexpr int U = L::kUnit, G = L::kGroup, kPairs = L::kUnits * U / 2;      // (f32x2 pairs of a half)
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int sub = lane / G, l = lane - sub * G;                  // head of the warp's kHeads, lane of the head
     const bool on = sub < L::kHeads;
     grid_launch_dependents();
     grid_dependency_wait();
-    struct Unit { int which, row, part, b, r, tok, before; };
+    // A unit is one token's heads of one tensor, or a share of them; it is gone through in rounds.  The list's entries are fetched a unit ahead
+    // of the copies.
+    struct Unit { int which, part, b, r, tok, before, h0, h1; };   // heads h0 .. h1 - 1; none behind the last unit
     auto unit_at = [&](int u) {
         Unit n = {};
         if (u >= p.units) return n;
         n.which = u >= p.units0 ? 1 : 0;
         const HeadTensor &t = p.t[n.which];
         const int v = n.which ? u - p.units0 : u;
-        n.row = t.parts == 1 ? v : v / t.parts; n.part = v - n.row * t.parts;
-        n.b = n.row / t.M; n.r = n.row - n.b * t.M;
-        n.tok = t.idx ? __ldcg(t.idx + n.row) : n.r;
-        n.before = (t.idx && n.r > 0) ? __ldcg(t.idx + n.row - 1) : -1;
+        const int row = t.parts == 1 ? v : v / t.parts;
+        n.part = v - row * t.parts;
+        n.b = row / t.M; n.r = row - n.b * t.M;
+        n.tok = t.idx ? __ldcg(t.idx + row) : n.r;
+        n.before = (t.idx && n.r > 0) ? __ldcg(t.idx + row - 1) : -1;
+        n.h0 = n.part * t.part_heads; n.h1 = min(t.H, n.h0 + t.part_heads);
         return n;
     };
-    int u = blockIdx.x * kWarps + warp;
-    Unit next = unit_at(u);                                        // list entries are fetched a token ahead
-    for (; u < p.units; u += gridDim.x * kWarps) {
-        const int which = next.which, part = next.part, b = next.b, r = next.r, tok = next.tok, before = next.before;
-        const HeadTensor &t = p.t[which];
-        next = unit_at(u + gridDim.x * kWarps);
-        if ((unsigned)tok >= (unsigned)p.N || before >= tok) {     // see astraea_scatter_reuse
-            if (lane == 0 && part == 0 && p.err_word) atomicExch(p.err_word, kErrBadIndex);
-            continue;
-        }
-        const __nv_bfloat16 *src = t.x + b * t.x_sb + (int64_t)(t.compact_in ? r : tok) * t.x_sn + l * U;
-        __nv_bfloat16 *dst = t.y + b * t.y_sb + (int64_t)(t.compact_out ? r : tok) * t.y_sn + l * U;
-        const int h0 = part * t.part_heads, h1 = min(t.H, h0 + t.part_heads);
-        // the first round of heads is sent for before the tables are
-        uint32_t raw[L::kUnroll][2][kPairs];
-        auto fetch = [&](int hb) {
+    auto bad = [&](const Unit &n) { return (unsigned)n.tok >= (unsigned)p.N || n.before >= n.tok; };      // see astraea_scatter_reuse
+    using R = Round<DH>;
+    extern __shared__ __align__(16) uint8_t smem[];
+    const uint8_t *rounds = smem + warp * (2 * R::kBytes);
+    const uint32_t s_rounds = static_cast<uint32_t>(__cvta_generic_to_shared(rounds));
+    auto send = [&](const Unit &n, int h0, int slot) {
+        if (h0 < n.h1 && !bad(n)) {
+            const HeadTensor &t = p.t[n.which];
+            const __nv_bfloat16 *src = t.x + n.b * t.x_sb + (int64_t)(t.compact_in ? n.r : n.tok) * t.x_sn + h0 * t.x_sh;
+            const uint32_t to = s_rounds + slot * R::kBytes;
+            const int left = n.h1 - h0;
 #pragma unroll
-            for (int k = 0; k < L::kUnroll; ++k) {
-                const int h = hb + k * L::kHeads;
-                if (on && h < h1) {
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int j = 0; j < L::kUnits; ++j) load_unit<U>(src + h * t.x_sh + s * (DH / 2) + G * j * U, &raw[k][s][j * (U / 2)]);
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kPairs; ++i) raw[k][0][i] = raw[k][1][i] = 0u;
-                }
+            for (int i = 0; i < (R::kVecs + 31) / 32; ++i) {
+                const int c = lane + 32 * i, head = c / R::kHeadVecs;
+                if (c < R::kVecs && head < left) copy_async(to + c * 16, src + head * t.x_sh + (c - head * R::kHeadVecs) * 8);
             }
-        };
-        fetch(h0 + sub);
-        // y = r (x by + x' cross) + plus for channel pairs x and their partners x': by = weight cos, cross = -+ partner's weight sin
-        f32x2 by[2][kPairs], cross[2][kPairs], plus[2][LAYER ? kPairs : 1];
-        {
-            const bool turned = on && tok < p.n_rot;
-            const float *pc = p.cos + (size_t)(turned ? tok : 0) * (DH / 2), *ps = p.sin + (size_t)(turned ? tok : 0) * (DH / 2);
-#pragma unroll
-            for (int j = 0; j < L::kUnits; ++j) {
-                const int c0 = (l + G * j) * U;                    // first channel of the access, in its half
-                uint32_t ww[2][U / 2], wb[2][U / 2];
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-#pragma unroll
-                    for (int i = 0; i < U / 2; ++i) { ww[s][i] = 0x3F803F80u; wb[s][i] = 0u; }
-                    if (on && t.weight) load_unit<U>(t.weight + s * (DH / 2) + c0, ww[s]);
-                    if (LAYER && on && t.bias) load_unit<U>(t.bias + s * (DH / 2) + c0, wb[s]);
-                }
-                float co[U], si[U];                                // HALF: of the channels; else of the pairs of both halves
-#pragma unroll
-                for (int i = 0; i < U; ++i) { co[i] = 1.f; si[i] = 0.f; }
-                if (turned) {
-                    if (HALF) { load_table<U>(pc + c0, co); load_table<U>(ps + c0, si); }
-                    else {
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            load_table<U / 2>(pc + s * (DH / 4) + c0 / 2, co + s * (U / 2));
-                            load_table<U / 2>(ps + s * (DH / 4) + c0 / 2, si + s * (U / 2));
-                        }
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < U / 2; ++i) {
-                    const int k = j * (U / 2) + i;
-                    if (HALF) {
-                        const f32x2 c = pack2(co[2 * i], co[2 * i + 1]), n = pack2(si[2 * i], si[2 * i + 1]), m = pack2(-si[2 * i], -si[2 * i + 1]);
-                        by[0][k] = mul2(widen(ww[0][i]), c); cross[0][k] = mul2(widen(ww[1][i]), m);
-                        by[1][k] = mul2(widen(ww[1][i]), c); cross[1][k] = mul2(widen(ww[0][i]), n);
-                        if (LAYER) {
-                            plus[0][LAYER ? k : 0] = fma2(widen(wb[0][i]), c, mul2(widen(wb[1][i]), m));
-                            plus[1][LAYER ? k : 0] = fma2(widen(wb[1][i]), c, mul2(widen(wb[0][i]), n));
-                        }
-                    } else {
-#pragma unroll
-                        for (int s = 0; s < 2; ++s) {
-                            const f32x2 c = twice(co[s * (U / 2) + i]), n = pack2(-si[s * (U / 2) + i], si[s * (U / 2) + i]);
-                            by[s][k] = mul2(widen(ww[s][i]), c); cross[s][k] = mul2(swapped(ww[s][i]), n);
-                            if (LAYER) plus[s][LAYER ? k : 0] = fma2(widen(wb[s][i]), c, mul2(swapped(wb[s][i]), n));
-                        }
-                    }
-                }
+            if (h0 == n.h0 && n.tok < p.n_rot && lane < 2 * R::kTableVecs) {
+                const float *table = lane < R::kTableVecs ? p.cos : p.sin;
+                copy_async(to + (R::kVecs + lane) * 16, table + (size_t)n.tok * (DH / 2) + (lane % R::kTableVecs) * 4);
             }
         }
-        for (int hb = h0 + sub; hb - sub < h1; hb += L::kUnroll * L::kHeads) {
-            if (hb != h0 + sub) fetch(hb);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int held = -1;                                                 // tensor whose weights are held
+    f32x2 w[2][kPairs], bi[2][LAYER ? kPairs : 1];
+    float co[kPairs * 2], si[kPairs * 2];                          // HALF: of the lane's channels; else of the pairs of both of its halves
+    const int stride = gridDim.x * kWarps;
+    int u = blockIdx.x * kWarps + warp, slot = 0;
+    Unit now = unit_at(u), ahead = unit_at(u + stride);
+    int hr = now.h0;                                               // first head of the round
+    send(now, hr, 0);
+    while (u < p.units) {
+        Unit next = now;
+        int next_hr = hr + R::kHeads, next_u = u;
+        if (next_hr >= now.h1 || bad(now)) {
+            next_u = u + stride;
+            next = ahead; next_hr = next.h0;
+            ahead = unit_at(next_u + stride);
+        }
+        __syncwarp();                                              // the other slot has been read by all lanes
+        send(next, next_hr, slot ^ 1);
+        asm volatile("cp.async.wait_group 1;" ::: "memory");
+        __syncwarp();
+        if (bad(now)) {
+            if (lane == 0 && now.part == 0 && p.err_word) atomicExch(p.err_word, kErrBadIndex);
+        } else {
+            const HeadTensor &t = p.t[now.which];
+            const uint8_t *mine = rounds + slot * R::kBytes;
+            if (now.which != held) {
+                held = now.which;
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int j = 0; j < L::kUnits; ++j) {
+                        uint32_t ww[U / 2], wb[U / 2];
+#pragma unroll
+                        for (int i = 0; i < U / 2; ++i) { ww[i] = 0x3F803F80u; wb[i] = 0u; }       // ones, zeros
+                        const int c = s * (DH / 2) + (l + G * j) * U;
+                        if (on && t.weight) load_unit<U>(t.weight + c, ww);
+                        if (LAYER && on && t.bias) load_unit<U>(t.bias + c, wb);
+#pragma unroll
+                        for (int i = 0; i < U / 2; ++i) {
+                            w[s][j * (U / 2) + i] = widen(ww[i]);
+                            if (LAYER) bi[s][LAYER ? j * (U / 2) + i : 0] = widen(wb[i]);
+                        }
+                    }
+            }
+            if (hr == now.h0) {                                     // a new token's angles
+                const bool turned = on && now.tok < p.n_rot;
+                const float *pc = reinterpret_cast<const float *>(mine + R::kVecs * 16), *ps = pc + DH / 2;
+#pragma unroll
+                for (int j = 0; j < L::kUnits; ++j)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int c0 = (l + G * j) * U;             // first channel of the access, in its half
+                        const int from = HALF ? c0 + s * (U / 2) : s * (DH / 4) + c0 / 2, to = HALF ? j * U + s * (U / 2) : s * kPairs + j * (U / 2);
+#pragma unroll
+                        for (int i = 0; i < U / 2; ++i) { co[to + i] = turned ? pc[from + i] : 1.f; si[to + i] = turned ? ps[from + i] : 0.f; }
+                    }
+            }
+            __nv_bfloat16 *dst = t.y + now.b * t.y_sb + (int64_t)(t.compact_out ? now.r : now.tok) * t.y_sn + l * U;
+            const int hb = hr + sub, h1 = now.h1;
 #pragma unroll
             for (int k = 0; k < L::kUnroll; ++k) {
                 const int h = hb + k * L::kHeads;
                 if (h - sub >= h1) break;                          // the whole warp: no head of this step is left
+                uint32_t raw[2][kPairs];
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int j = 0; j < L::kUnits; ++j) {
+                        const uint8_t *at = mine + (k * L::kHeads + (on ? sub : 0)) * (DH * 2) + s * DH + (l + G * j) * (U * 2);
+                        uint32_t *to = &raw[s][j * (U / 2)];
+                        if constexpr (U == 8) { const uint4 v = *reinterpret_cast<const uint4 *>(at); to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w; }
+                        else { const uint2 v = *reinterpret_cast<const uint2 *>(at); to[0] = v.x; to[1] = v.y; }
+                    }
                 f32x2 z[2][kPairs];
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int i = 0; i < kPairs; ++i) z[s][i] = widen(raw[k][s][i]);
+                    for (int i = 0; i < kPairs; ++i) z[s][i] = widen(raw[s][i]);
                 float lo, hi;
                 if (LAYER) {
                     f32x2 a = 0ull;
@@ -223,12 +240,23 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
                 unpack2(a, lo, hi);
                 const f32x2 rstd = twice(rsqrtf(group_sum<G>(lo + hi, lane) * (1.0f / DH) + p.eps));
 #pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        z[s][i] = mul2(z[s][i], rstd);
+                        z[s][i] = LAYER ? fma2(z[s][i], w[s][i], bi[s][LAYER ? i : 0]) : mul2(z[s][i], w[s][i]);
+                    }
+#pragma unroll
                 for (int i = 0; i < kPairs; ++i) {
                     const f32x2 x0 = z[0][i], x1 = z[1][i];
-                    z[0][i] = fma2(x0, by[0][i], mul2(HALF ? x1 : swapped(x0), cross[0][i]));
-                    z[1][i] = fma2(x1, by[1][i], mul2(HALF ? x0 : swapped(x1), cross[1][i]));
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) z[s][i] = LAYER ? fma2(z[s][i], rstd, plus[s][LAYER ? i : 0]) : mul2(z[s][i], rstd);
+                    if (HALF) {
+                        const f32x2 c = pack2(co[2 * i], co[2 * i + 1]);
+                        z[0][i] = fma2(x0, c, mul2(x1, pack2(-si[2 * i], -si[2 * i + 1])));
+                        z[1][i] = fma2(x1, c, mul2(x0, pack2(si[2 * i], si[2 * i + 1])));
+                    } else {
+                        z[0][i] = fma2(x0, twice(co[i]), mul2(swapped(x0), pack2(-si[i], si[i])));
+                        z[1][i] = fma2(x1, twice(co[kPairs + i]), mul2(swapped(x1), pack2(-si[kPairs + i], si[kPairs + i])));
+                    }
                 }
                 if (on && h < h1) {
 #pragma unroll
@@ -238,6 +266,8 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
                 }
             }
         }
+        now = next; hr = next_hr; u = next_u;
+        slot ^= 1;
     }
 }
 
@@ -268,7 +298,16 @@ int32_t launch_dim(HeadNormParams &p, const astraea_head_rows *rows, int n, int 
     const int grid = (int)(want < cap ? want : cap);
     auto kernel = layer ? (half ? head_norm_kernel<DH, true, true> : head_norm_kernel<DH, true, false>)
                         : (half ? head_norm_kernel<DH, false, true> : head_norm_kernel<DH, false, false>);
-    launch_overlapped(kernel, grid, kWarps * 32, 0, stream, p);
+    constexpr int kSmem = kWarps * 2 * Round<DH>::kBytes;           // 52 KB at head_dim 128
+    static PerDeviceOnce attrs;                   // the attribute is per device (all four kernels of the width at once)
+    if (attrs.run([] {
+            cudaError_t e = cudaSuccess;
+            for (auto k : {head_norm_kernel<DH, true, true>, head_norm_kernel<DH, true, false>, head_norm_kernel<DH, false, true>, head_norm_kernel<DH, false, false>})
+                if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+            return e;
+        }) != cudaSuccess)
+        return check_launch("astraea_qk_norm_rotate (shared memory attribute)");
+    launch_overlapped(kernel, grid, kWarps * 32, kSmem, stream, p);
     return check_launch("astraea_qk_norm_rotate");
 }
 
