@@ -114,7 +114,9 @@ template <int DH, int TM, bool WIN = false> struct Cfg {
     // no faster than the XU in any share (0 / 1 / 2 / 3 of eight pairs: 3276 x 65536 x 24 heads 2128 / 2117 / 2149 / 2227,
     // 35640 x 118800 x 24 40200 / 40300 / 40700 / 42300).
     static constexpr int kPolyPeriod = (DH == 72 && TM == 2) ? 4 : 8;
-    static constexpr int kPolyPairs = (DH == 72) ? 1 : (DH == 64) ? 3 : 0;
+    // Nor any in windows: their rows may have few terms, whose sums the cubic's 8.6e-5 does not average out of, and their loops have the time
+    // (us without / with: 4613 of 17776 x 24 heads of 64 over 2048 keys either way 231 / 243, over 8000 523 / 542; the Open-Sora shape 485 / 486).
+    static constexpr int kPolyPairs = WIN ? 0 : (DH == 72) ? 1 : (DH == 64) ? 3 : 0;
     static constexpr int kSoftmaxWarps = 4 * kTilesM * kSplit;
     static constexpr int kAhead = kSBufs;                         // Q K^T runs this many key tiles ahead of P V
     static constexpr int kThreads = (kSoftmaxWarps + 4) * 32;     // + producer, two issuers, one register donor

@@ -77,6 +77,11 @@ template <int U> __device__ __forceinline__ void store_unit(__nv_bfloat16 *p, co
     if constexpr (U == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
     else *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
 }
+// N consecutive values of a table
+template <int N> __device__ __forceinline__ void load_table(const float *p, float *f) {
+    if constexpr (N == 2) asm volatile("ld.global.v2.f32 {%0,%1}, [%2];" : "=f"(f[0]), "=f"(f[1]) : "l"(p));
+    else asm volatile("ld.global.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f[0]), "=f"(f[1]), "=f"(f[2]), "=f"(f[3]) : "l"(p));
+}
 __device__ __forceinline__ f32x2 widen(uint32_t w) { return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 __device__ __forceinline__ f32x2 swapped(f32x2 v) { float lo, hi; unpack2(v, lo, hi); return pack2(hi, lo); }
 __device__ __forceinline__ f32x2 twice(float v) { return pack2(v, v); }
@@ -91,6 +96,73 @@ template <int G> __device__ __forceinline__ float group_sum(float s, int lane) {
         for (int o = G / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         return s;
     }
+}
+
+// The weights and biases of a lane's channels.
+template <int DH, bool LAYER, int PAIRS, int BIAS>
+__device__ __forceinline__ void load_weights(const HeadTensor &t, int l, bool on, f32x2 (&w)[2][PAIRS], f32x2 (&bi)[2][BIAS])
+{
+    using L = Lanes<DH>;
+    constexpr int U = L::kUnit, G = L::kGroup;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int j = 0; j < L::kUnits; ++j) {
+                            uint32_t ww[U / 2], wb[U / 2];
+#pragma unroll
+                            for (int i = 0; i < U / 2; ++i) { ww[i] = 0x3F803F80u; wb[i] = 0u; }       // ones, zeros
+                            const int c = s * (DH / 2) + (l + G * j) * U;
+                            if (on && t.weight) load_unit<U>(t.weight + c, ww);
+                            if (LAYER && on && t.bias) load_unit<U>(t.bias + c, wb);
+#pragma unroll
+                            for (int i = 0; i < U / 2; ++i) {
+                                w[s][j * (U / 2) + i] = widen(ww[i]);
+                                if (LAYER) bi[s][LAYER ? j * (U / 2) + i : 0] = widen(wb[i]);
+                            }
+                        }
+}
+// A head: z is a lane's channels of its first and second half; co and si the cosines and sines of its channels (HALF) or of its pairs.
+template <int DH, bool LAYER, bool HALF, int PAIRS, int BIAS>
+__device__ __forceinline__ void norm_rotate(f32x2 (&z)[2][PAIRS], const f32x2 (&w)[2][PAIRS], const f32x2 (&bi)[2][BIAS], const float (&co)[2 * PAIRS],
+                                            const float (&si)[2 * PAIRS], float eps, int lane)
+{
+    constexpr int G = Lanes<DH>::kGroup, kPairs = PAIRS;
+                    float lo, hi;
+                    if (LAYER) {
+                        f32x2 a = 0ull;
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) a = add2(a, add2(z[0][i], z[1][i]));
+                        unpack2(a, lo, hi);
+                        const f32x2 minus_mean = twice(group_sum<G>(lo + hi, lane) * (-1.0f / DH));
+#pragma unroll
+                        for (int s = 0; s < 2; ++s)
+#pragma unroll
+                            for (int i = 0; i < kPairs; ++i) z[s][i] = add2(z[s][i], minus_mean);
+                    }
+                    f32x2 a = 0ull;
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) a = fma2(z[1][i], z[1][i], fma2(z[0][i], z[0][i], a));
+                    unpack2(a, lo, hi);
+                    const f32x2 rstd = twice(rsqrtf(group_sum<G>(lo + hi, lane) * (1.0f / DH) + eps));
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) {
+                            z[s][i] = mul2(z[s][i], rstd);
+                            z[s][i] = LAYER ? fma2(z[s][i], w[s][i], bi[s][LAYER ? i : 0]) : mul2(z[s][i], w[s][i]);
+                        }
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        const f32x2 x0 = z[0][i], x1 = z[1][i];
+                        if (HALF) {
+                            const f32x2 c = pack2(co[2 * i], co[2 * i + 1]);
+                            z[0][i] = fma2(x0, c, mul2(x1, pack2(-si[2 * i], -si[2 * i + 1])));
+                            z[1][i] = fma2(x1, c, mul2(x0, pack2(si[2 * i], si[2 * i + 1])));
+                        } else {
+                            z[0][i] = fma2(x0, twice(co[i]), mul2(swapped(x0), pack2(-si[i], si[i])));
+                            z[1][i] = fma2(x1, twice(co[kPairs + i]), mul2(swapped(x1), pack2(-si[kPairs + i], si[kPairs + i])));
+                        }
+                    }
 }
 
 // LAYER: layer norm with a bias (RMS norm without one otherwise); HALF: channels are paired (p, p + DH/2) and not (2p, 2p + 1)
@@ -171,22 +243,7 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
             const uint8_t *mine = rounds + slot * R::kBytes;
             if (now.which != held) {
                 held = now.which;
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int j = 0; j < L::kUnits; ++j) {
-                        uint32_t ww[U / 2], wb[U / 2];
-#pragma unroll
-                        for (int i = 0; i < U / 2; ++i) { ww[i] = 0x3F803F80u; wb[i] = 0u; }       // ones, zeros
-                        const int c = s * (DH / 2) + (l + G * j) * U;
-                        if (on && t.weight) load_unit<U>(t.weight + c, ww);
-                        if (LAYER && on && t.bias) load_unit<U>(t.bias + c, wb);
-#pragma unroll
-                        for (int i = 0; i < U / 2; ++i) {
-                            w[s][j * (U / 2) + i] = widen(ww[i]);
-                            if (LAYER) bi[s][LAYER ? j * (U / 2) + i : 0] = widen(wb[i]);
-                        }
-                    }
+                load_weights<DH, LAYER>(t, l, on, w, bi);
             }
             if (hr == now.h0) {                                     // a new token's angles
                 const bool turned = on && now.tok < p.n_rot;
@@ -222,42 +279,7 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) z[s][i] = widen(raw[s][i]);
-                float lo, hi;
-                if (LAYER) {
-                    f32x2 a = 0ull;
-#pragma unroll
-                    for (int i = 0; i < kPairs; ++i) a = add2(a, add2(z[0][i], z[1][i]));
-                    unpack2(a, lo, hi);
-                    const f32x2 minus_mean = twice(group_sum<G>(lo + hi, lane) * (-1.0f / DH));
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int i = 0; i < kPairs; ++i) z[s][i] = add2(z[s][i], minus_mean);
-                }
-                f32x2 a = 0ull;
-#pragma unroll
-                for (int i = 0; i < kPairs; ++i) a = fma2(z[1][i], z[1][i], fma2(z[0][i], z[0][i], a));
-                unpack2(a, lo, hi);
-                const f32x2 rstd = twice(rsqrtf(group_sum<G>(lo + hi, lane) * (1.0f / DH) + p.eps));
-#pragma unroll
-                for (int s = 0; s < 2; ++s)
-#pragma unroll
-                    for (int i = 0; i < kPairs; ++i) {
-                        z[s][i] = mul2(z[s][i], rstd);
-                        z[s][i] = LAYER ? fma2(z[s][i], w[s][i], bi[s][LAYER ? i : 0]) : mul2(z[s][i], w[s][i]);
-                    }
-#pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    const f32x2 x0 = z[0][i], x1 = z[1][i];
-                    if (HALF) {
-                        const f32x2 c = pack2(co[2 * i], co[2 * i + 1]);
-                        z[0][i] = fma2(x0, c, mul2(x1, pack2(-si[2 * i], -si[2 * i + 1])));
-                        z[1][i] = fma2(x1, c, mul2(x0, pack2(si[2 * i], si[2 * i + 1])));
-                    } else {
-                        z[0][i] = fma2(x0, twice(co[i]), mul2(swapped(x0), pack2(-si[i], si[i])));
-                        z[1][i] = fma2(x1, twice(co[kPairs + i]), mul2(swapped(x1), pack2(-si[kPairs + i], si[kPairs + i])));
-                    }
-                }
+                norm_rotate<DH, LAYER, HALF>(z, w, bi, co, si, p.eps, lane);
                 if (on && h < h1) {
 #pragma unroll
                     for (int s = 0; s < 2; ++s)
@@ -271,9 +293,90 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
     }
 }
 
-template <int DH>
-int32_t launch_dim(HeadNormParams &p, const astraea_head_rows *rows, int n, int B, bool layer, bool half, cudaStream_t stream)
+// Tensors of few heads (keys that many query heads share): a warp's lanes hold heads of several tokens, each with angles of its own, two steps
+// of them in flight.  A warp for each token would leave most of its lanes idle.
+template <int DH, bool LAYER, bool HALF>
+__global__ void __launch_bounds__(kWarps * 32, 3) few_heads_kernel(const __grid_constant__ HeadNormParams p, int which, int B)
 {
+    using L = Lanes<DH>;
+    constexpr int U = L::kUnit, G = L::kGroup, kPairs = L::kUnits * U / 2, kSteps = 2;
+    const int lane = threadIdx.x & 31, sub = lane / G, l = lane - sub * G;
+    const bool on = sub < L::kHeads;
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const HeadTensor &t = p.t[which];
+    const long long rows = (long long)B * t.M * t.H;               // (token, head) pairs
+    f32x2 w[2][kPairs], bi[2][LAYER ? kPairs : 1];
+    load_weights<DH, LAYER>(t, l, on, w, bi);
+    const long long step = (long long)gridDim.x * kWarps * kSteps * L::kHeads;
+    for (long long base = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kSteps * L::kHeads; base < rows; base += step) {
+        uint32_t raw[kSteps][2][kPairs];
+        float co[kSteps][kPairs * 2], si[kSteps][kPairs * 2];
+        __nv_bfloat16 *dst[kSteps];
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            const long long row = base + k * L::kHeads + sub;
+            const bool there = on && row < rows;
+            const int token = there ? (int)(row / t.H) : 0, h = there ? (int)(row - (long long)token * t.H) : 0;      // (fewer than 2^30 tokens)
+            const int b = token / t.M, r = token - b * t.M;
+            const int tok = t.idx ? __ldcg(t.idx + token) : r, before = t.idx && r > 0 ? __ldcg(t.idx + token - 1) : -1;
+            const bool bad = (unsigned)tok >= (unsigned)p.N || before >= tok;                      // see astraea_scatter_reuse
+            if (there && bad && h == 0 && l == 0 && p.err_word) atomicExch(p.err_word, kErrBadIndex);
+            const bool good = there && !bad;
+            dst[k] = good ? t.y + b * t.y_sb + (int64_t)(t.compact_out ? r : tok) * t.y_sn + h * t.y_sh + l * U : nullptr;
+            const __nv_bfloat16 *src = good ? t.x + b * t.x_sb + (int64_t)(t.compact_in ? r : tok) * t.x_sn + h * t.x_sh + l * U : nullptr;
+            const bool turned = good && tok < p.n_rot;
+            const float *pc = p.cos + (size_t)(turned ? tok : 0) * (DH / 2), *ps = p.sin + (size_t)(turned ? tok : 0) * (DH / 2);
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int j = 0; j < L::kUnits; ++j) {
+#pragma unroll
+                    for (int i = 0; i < U / 2; ++i) raw[k][s][j * (U / 2) + i] = 0u;
+                    if (good) load_unit<U>(src + s * (DH / 2) + G * j * U, &raw[k][s][j * (U / 2)]);
+                    const int c0 = (l + G * j) * U;                 // first channel of the access, in its half
+                    const int from = HALF ? c0 + s * (U / 2) : s * (DH / 4) + c0 / 2, to = HALF ? j * U + s * (U / 2) : s * kPairs + j * (U / 2);
+#pragma unroll
+                    for (int i = 0; i < U / 2; ++i) { co[k][to + i] = 1.f; si[k][to + i] = 0.f; }
+                    if (turned) { load_table<U / 2>(pc + from, &co[k][to]); load_table<U / 2>(ps + from, &si[k][to]); }
+                }
+        }
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) {
+            f32x2 z[2][kPairs];
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) z[s][i] = widen(raw[k][s][i]);
+            norm_rotate<DH, LAYER, HALF>(z, w, bi, co[k], si[k], p.eps, lane);
+            if (dst[k]) {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int j = 0; j < L::kUnits; ++j) store_unit<U>(dst[k] + s * (DH / 2) + G * j * U, &z[s][j * (U / 2)]);
+            }
+        }
+    }
+}
+
+template <int DH>
+int32_t launch_dim(HeadNormParams &p, int n, int B, bool layer, bool half, cudaStream_t stream)
+{
+    // a tensor of few heads and many tokens goes by itself (a short one is not worth a launch of its own)
+    bool alone[2] = {false, false};
+    for (int i = 0; i < n; ++i) alone[i] = p.t[i].H <= Lanes<DH>::kHeads && (long long)B * p.t[i].M > (long long)sm_count() * 64;
+    for (int i = 0; i < n; ++i) {
+        if (!alone[i]) continue;
+        const long long want = ((long long)B * p.t[i].M * p.t[i].H + kWarps * 2 * Lanes<DH>::kHeads - 1) / (kWarps * 2 * Lanes<DH>::kHeads), cap = (long long)sm_count() * 12;
+        auto kernel = layer ? (half ? few_heads_kernel<DH, true, true> : few_heads_kernel<DH, true, false>)
+                            : (half ? few_heads_kernel<DH, false, true> : few_heads_kernel<DH, false, false>);
+        launch_overlapped(kernel, (int)(want < cap ? want : cap), kWarps * 32, 0, stream, p, i, B);
+        const int32_t rc = check_launch("astraea_qk_norm_rotate");
+        if (rc != ASTRAEA_OK) return rc;
+    }
+    if (alone[0]) { p.t[0] = p.t[1]; alone[0] = alone[1]; --n; }
+    if (n == 2 && alone[1]) n = 1;
+    if (n == 0 || (n == 1 && alone[0])) return ASTRAEA_OK;
     // A token's heads go to one warp where that gives every SM its 32 warps, and are shared out in steps of a warp's heads where it does
     // not: one token of 32 + 8 heads is then 10 warps and not 2.
     long long all_rows = 0;
@@ -332,9 +435,9 @@ int32_t launch_qk_norm_rotate(const astraea_head_rows *rows, int n, const float 
     }
     p.cos = cos; p.sin = sin; p.n_rot = n_rot; p.N = N; p.eps = eps; p.err_word = err_word;
     switch (d) {
-    case 64: return launch_dim<64>(p, rows, n, B, layer, half, stream);
-    case 72: return launch_dim<72>(p, rows, n, B, layer, half, stream);
-    default: return launch_dim<128>(p, rows, n, B, layer, half, stream);
+    case 64: return launch_dim<64>(p, n, B, layer, half, stream);
+    case 72: return launch_dim<72>(p, n, B, layer, half, stream);
+    default: return launch_dim<128>(p, n, B, layer, half, stream);
     }
 }
 

@@ -137,6 +137,51 @@ def test_bad_entries_are_skipped_and_reported_and_nan_stays_in_its_head():
     assert bool((y == 7).all())
 
 
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("norm", [A.NORM_RMS, A.NORM_LAYER])
+@pytest.mark.parametrize("rotation", [A.ROTATE_INTERLEAVED, A.ROTATE_HALF])
+@pytest.mark.parametrize("H,H_kv", [(8, 1), (2, 1), (1, 16)])
+def test_few_heads_of_many_tokens(d, norm, rotation, H, H_kv):
+    g = torch.Generator("cuda").manual_seed(d + H)
+    B, N, M, n_rot = 2, 6007, 5001, 5990
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()
+    q, k, wq, wk = 3 * rnd(B, N, H, d), 3 * rnd(B, N, H_kv, d), 1 + 0.3 * rnd(d), rnd(d)
+    bk = rnd(d) if norm == A.NORM_LAYER else None
+    cos, sin = table(n_rot, d, g)
+    idx = torch.stack([torch.randperm(N, device="cuda", generator=g)[:M].sort().values for _ in range(B)]).int()
+    idx[1, 77] = idx[1, 76]                                        # a row that is skipped
+    before = rnd(B, N, H, d)
+    qo, ko = Guarded((B, N, H, d), torch.bfloat16, before), Guarded((B, N, H_kv, d), torch.bfloat16)
+    ws = A.new_workspace(A.OP_QK_NORM_ROTATE, B, H, N, M, d)
+    sq, sk = A.bhnd_strides(N, H, d), A.bhnd_strides(N, H_kv, d)
+    A.astraea_qk_norm_rotate([A.head_rows(q, sq, qo.t, sq, H, idx, M, wq), A.head_rows(k, sk, ko.t, sk, H_kv, weight=wk, bias=bk)], cos, sin, n_rot,
+                             B, N, d, norm, rotation, EPS, ws)
+    with pytest.raises(A.AstraeaError) as e:
+        A.astraea_poll_error(ws)
+    assert e.value.code == A.ERR_BAD_INDEX
+
+    def want(x, w, b):
+        x = x.double() - (x.double().mean(-1, keepdim=True) if norm == A.NORM_LAYER else 0)
+        z = x / ((x * x).mean(-1, keepdim=True) + EPS).sqrt() * w.double() + (0 if b is None else b.double())
+        c, s = torch.ones(N, d // 2, device="cuda", dtype=torch.float64), torch.zeros(N, d // 2, device="cuda", dtype=torch.float64)
+        c[:n_rot], s[:n_rot] = cos.double(), sin.double()
+        c, s = c[None, :, None], s[None, :, None]
+        if rotation == A.ROTATE_HALF:
+            u, v = z.chunk(2, -1)
+            return torch.cat([u * c - v * s, u * s + v * c], -1), z
+        u, v = z[..., 0::2], z[..., 1::2]
+        return torch.stack([u * c - v * s, u * s + v * c], -1).flatten(-2), z
+
+    y, z = want(k, wk, bk)
+    close(ko.t, y, z, norm == A.NORM_LAYER)
+    y, z = want(q, wq, None)
+    rows = torch.zeros(B, N, dtype=torch.bool, device="cuda")
+    rows[torch.arange(B, device="cuda")[:, None], idx.long()] = True
+    close(qo.t[rows], y[rows], z[rows], norm == A.NORM_LAYER)
+    assert torch.equal(qo.t[~rows], before[~rows])
+    qo.check(); ko.check()
+
+
 def test_many_rows_and_another_stream():
     g = torch.Generator("cuda").manual_seed(3)
     B, N, H, d = 1, 4999, 24, 128                                  # more rows than warps: every warp takes several
