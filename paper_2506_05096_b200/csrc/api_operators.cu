@@ -64,6 +64,7 @@ int32_t astraea_qk_norm_rotate(const astraea_head_rows *rows, int n, const float
     const char *fn = "astraea_qk_norm_rotate";
     REQUIRE(rows && (n == 1 || n == 2), "%s: one or two tensors, got %d", fn, rows ? n : 0);
     REQUIRE(B > 0 && N > 0, "%s: B and N must be positive", fn);
+    REQUIRE((long long)B * N <= 1 << 30, "%s: too many rows", fn);
     if (d != 64 && d != 72 && d != 128) return fail(ASTRAEA_ERR_UNSUPPORTED, "%s: head_dim %d not in {64, 72, 128}", fn, d);
     if (norm != ASTRAEA_NORM_RMS && norm != ASTRAEA_NORM_LAYER) return fail(ASTRAEA_ERR_UNSUPPORTED, "%s: unknown norm %d", fn, norm);
     if (rotation != ASTRAEA_ROTATE_INTERLEAVED && rotation != ASTRAEA_ROTATE_HALF) return fail(ASTRAEA_ERR_UNSUPPORTED, "%s: unknown rotation %d", fn, rotation);

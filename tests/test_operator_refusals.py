@@ -28,7 +28,7 @@ def test_head_norm(L):
     assert call(rows(), d=80) == A.ERR_UNSUPPORTED
     assert call(rows(), norm=2) == A.ERR_UNSUPPORTED and call(rows(), rotation=-1) == A.ERR_UNSUPPORTED
     assert call(rows(flags=4)) == A.ERR_UNSUPPORTED
-    for bad in (dict(n_rot=17), dict(n_rot=-1), dict(cos=None), dict(sin=P + 4), dict(eps=-1.0), dict(ws=2), dict(B=0), dict(N=0)):
+    for bad in (dict(n_rot=17), dict(n_rot=-1), dict(cos=None), dict(sin=P + 4), dict(eps=-1.0), dict(ws=2), dict(B=0), dict(N=0), dict(B=1 << 11, N=1 << 20)):
         assert call(rows(), **bad) == A.ERR_INVALID_ARG, bad
     for bad in (dict(x=None), dict(y=None), dict(x=P + 2), dict(y=P + 8), dict(H=0), dict(weight=P + 4), dict(bias=P), dict(idx=P, M=17),
                 dict(idx=P, M=-1), dict(flags=A.ROWS_COMPACT_IN), dict(xs=(2048, 64, 132)), dict(ys=(2048, 32, 128)), dict(xs=(-8, 64, 128))):
