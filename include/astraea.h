@@ -239,7 +239,7 @@ int32_t astraea_sparse_cross_attn(const void *q, const void *k, const void *v,
  *             stream's newest token against its cache: M = 1, q_idx its place, COMPACT_Q | COMPACT_OUT)
  *   k, v    : bf16 [B, N, H_kv, d] through their strides; keys that a row does not see, those from kv_len[b] on in
  *             particular, may hold anything, NaN included
- *   q_idx, M, out, lse_out, scale, flags : as astraea_sparse_attn; N at most 2^30
+ *   q_idx, M, out, lse_out, scale, flags : as astraea_sparse_attn; N and M H / H_kv at most 2^30, H at most 4096 H_kv
  *   kv_len  : int32 [B] keys that exist (values outside [0, N] count as the nearer end); NULL => N
  *   workspace : 256-byte aligned, at least 256 bytes; with astraea_workspace_bytes(ASTRAEA_OP_WINDOW_ATTN, B, H, N, M, d) the
  *             units of a last, partial round (all units of a small call) may be shared out by keys over 2..16 CTAs each.  A
@@ -373,7 +373,8 @@ int32_t astraea_layernorm_modulate(const void *x, const int32_t *idx, int M, con
  *   rows   : HOST array of n = 1 or 2 tensors (queries and keys, each with heads, lists and weights of its own) that go in
  *            one launch:
  *              x, y    bf16 heads, head_dim contiguous; element strides (batch, head, token) given per tensor, multiples of
- *                      8.  y may be x (with the same strides and both or neither compact); other overlaps are not allowed.
+ *                      8.  y may be x (with the same strides and both or neither compact); other overlaps are not allowed,
+ *                      nor are heads of y that overlap one another.  B N at most 2^30.
  *              idx, M  int32 [B, M] strictly ascending in [0, N); NULL => all N rows (M ignored, no compact flags)
  *              H       heads
  *              weight, bias  bf16 [d], shared by the heads; NULL => ones / zeros (bias with the layer norm only)
@@ -424,7 +425,7 @@ int32_t astraea_quantize_fp8_weight(const void *w, void *wq, float *w_scale, int
  *   flags    : ASTRAEA_LINEAR_COMPACT_OUT, _GELU, _COMPACT_RES as there (COMPACT_IN has nothing to say: xq is always compact)
  *   workspace : at least 256 bytes, 256-byte aligned, zero before the first use (the error word)
  * Products of a block exact, summed in fp32 by the tensor cores; scaled and summed over the blocks in fp32; one rounding to
- * bf16.  K a multiple of 128, N_out of 8; pointers 16-byte aligned (scales 4).  M = 0 is valid.  Bad index entries as there.
+ * bf16.  K a multiple of 128, N_out of 8 (up to 65535 * 128), B N up to 2^31 - 256; pointers 16-byte aligned (scales 4).  M = 0 is valid.  Bad index entries as there.
  * Errors: INVALID_ARG, UNSUPPORTED (unknown flags), WORKSPACE_TOO_SMALL, CUDA.
  */
 int32_t astraea_gathered_linear_fp8(const void *xq, const float *x_scale, const int32_t *idx, int M,

@@ -116,7 +116,7 @@ int32_t astraea_quantize_fp8_weight(const void *w, void *wq, float *w_scale, int
 {
     const char *fn = "astraea_quantize_fp8_weight";
     REQUIRE(N_out > 0 && K > 0 && K % 128 == 0, "%s: N_out must be positive, K=%d a positive multiple of 128", fn, K);
-    REQUIRE((N_out + 127) / 128 <= 65535, "%s: N_out=%d is too large", fn, N_out);
+    REQUIRE(N_out <= 65535 * 128, "%s: N_out=%d is too large", fn, N_out);
     REQUIRE(w && wq && w_scale, "%s: null w, wq or w_scale", fn);
     REQUIRE(aligned16(w) && aligned16(wq) && (reinterpret_cast<uintptr_t>(w_scale) & 3u) == 0, "%s: w and wq must be 16-byte aligned, w_scale 4-byte", fn);
     return launch_quantize_fp8_weight(w, wq, w_scale, N_out, K, (cudaStream_t)stream);
@@ -131,7 +131,7 @@ int32_t astraea_gathered_linear_fp8(const void *xq, const float *x_scale, const 
     REQUIRE(B > 0 && N > 0 && K > 0 && N_out > 0, "%s: B, N, K, N_out must be positive", fn);
     REQUIRE(!idx || (M >= 0 && M <= N), "%s: M=%d outside [0, N=%d]", fn, M, N);
     REQUIRE(K % 128 == 0, "%s: K=%d must be a multiple of 128", fn, K);
-    REQUIRE(N_out % 8 == 0, "%s: N_out=%d must be a multiple of 8", fn, N_out);
+    REQUIRE(N_out % 8 == 0 && N_out <= 65535 * 128, "%s: N_out=%d must be a multiple of 8 and is limited to 65535 * 128", fn, N_out);
     if (flags & ~(ASTRAEA_LINEAR_COMPACT_OUT | ASTRAEA_LINEAR_GELU | ASTRAEA_LINEAR_COMPACT_RES)) return fail(ASTRAEA_ERR_UNSUPPORTED, "%s: unknown flags 0x%x", fn, flags);
     REQUIRE(!(flags & (ASTRAEA_LINEAR_COMPACT_OUT | ASTRAEA_LINEAR_COMPACT_RES)) || idx, "%s: compact rows need an index list", fn);
     REQUIRE(!(flags & ASTRAEA_LINEAR_COMPACT_RES) || residual, "%s: ASTRAEA_LINEAR_COMPACT_RES without a residual", fn);

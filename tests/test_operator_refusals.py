@@ -94,3 +94,15 @@ def test_window_attention(L):
     # room for the key shares: one unit's at least, no more than 296 shares
     assert 256 + 16 * 256 * 516 <= L.astraea_workspace_bytes(A.OP_WINDOW_ATTN, 1, 1, 1000, 1, 128) < 3 << 20
     assert L.astraea_workspace_bytes(A.OP_WINDOW_ATTN, 8, 64, 1 << 20, 1 << 20, 128) < 40 << 20
+
+
+def test_sizes_at_the_limits(L):
+    assert L.astraea_quantize_fp8_weight(P, P, P, 65535 * 128 + 1, 128, None) == A.ERR_INVALID_ARG
+    assert L.astraea_quantize_fp8_weight(P, P, P, 0x7fffffff, 128, None) == A.ERR_INVALID_ARG
+    for n_out in (65535 * 128 + 8, 0x7ffffff8):
+        assert L.astraea_gathered_linear_fp8(P, P, P, 4, P, P, None, None, None, P, 1, 16, 128, n_out, 0, P, 256, None) == A.ERR_INVALID_ARG
+        assert b"65535" in L.astraea_last_error()
+    s = (1 << 20, 64, 128)
+    for h, h_kv in ((4097, 1), (8194, 2)):                 # query heads of a key head
+        assert L.astraea_window_attn(P, P, P, *s, *s, *s, P, 4, None, P, None, 1, h, h_kv, 16, 64, 0, 0, 1, 1, 0.0, 0, P, 256, None) == A.ERR_INVALID_ARG
+        assert b"4096" in L.astraea_last_error()
