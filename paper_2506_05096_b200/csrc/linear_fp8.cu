@@ -35,9 +35,10 @@ constexpr int kTileRows = 256, kRowsCta = kTileRows / 2, kBK = 128;    // bytes 
 constexpr int kSumWarps = 8;
 constexpr int kTmaWarp = kSumWarps, kMmaWarp = kTmaWarp + 1;
 constexpr int kThreads = (kSumWarps + 4) * 32;
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr int kABytes = kRowsCta * kBK, kBBytes = 128 * kBK;           // (B: half of at most 256 columns)
-constexpr int kStageBytes = 32 * 64;                                   // per sum warp: 32 rows x 32 bf16 columns on their way to / from global memory
+constexpr int kBufBytes = 32 * 64;                                     // 32 rows x 32 bf16 columns on their way to / from global memory
+constexpr int kStageBytes = 2 * kBufBytes;                             // per sum warp: two of them in turn
 constexpr int kMaxAcc = 4;
 constexpr int kAhead = 4;                                              // blocks between the load of a row's scale and its use
 constexpr int kBarBytes = 256;
@@ -57,6 +58,7 @@ struct Fp8Params {
     const __nv_bfloat16 *bias, *residual, *gate;
     __nv_bfloat16 *y;
     int compact, res_compact, gelu;
+    int whole;                           // the rows of y lie one behind the other: a warp's go out by TMA
     int *err_word;
 };
 
@@ -94,30 +96,37 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *m, 
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4}], [%2];"
         ::"r"(dst), "l"(m), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
-// gelu2 with one reciprocal for both elements, of the product of their divisors (1 .. 3 with |z| limited to 6, where the erf is one): three
-// XU operations a pair instead of four, which cost an epilogue more than anything else (13106 x 1152 x 4608: 80 us without the GELU, 110 with).
-__device__ __forceinline__ f32x2 gelu2_one_reciprocal(f32x2 x) {
-    float x0, x1, d0, d1, a0, a1, r, e0, e1;
-    unpack2(x, x0, x1);
-    const f32x2 az = pack2(fminf(fabsf(x0) * 0.70710678118654752f, 6.0f), fminf(fabsf(x1) * 0.70710678118654752f, 6.0f));       // |z|
-    unpack2(fma2(az, both(0.3275911f), both(1.0f)), d0, d1);
+// GELU(x) = x Phi(x) of two elements, Phi(x) = 1 / (1 + 2^-g(x)) with g the log2 of Phi(x) / Phi(-x): odd and smooth, x times a polynomial of degree six
+// in x^2 over |x| < 5.75 (fitted here for the least error of Phi: 5.4e-8 with fp32 arithmetic) and linear beyond, where Phi(-|x|) is below
+// 5e-9.  One reciprocal for both, of the product of their divisors (up to 2^60 each): three XU operations a pair instead of the four of
+// gelu2, and 23 clocks of the FMA pipe instead of 27, which an epilogue has more of than anything else.
+__device__ __forceinline__ f32x2 gelu2_odds(f32x2 x) {
+    float t0, t1, a0, a1, d0, d1, e0, e1, r;
+    unpack2(mul2(x, x), t0, t1);
+    const f32x2 t = pack2(fminf(t0, 33.0625f), fminf(t1, 33.0625f));
+    f32x2 g = fma2(both(-5.067235e-9f), t, both(3.8163125e-7f));                          // minus the polynomial
+    g = fma2(g, t, both(-1.1439834e-5f));
+    g = fma2(g, t, both(1.5957994e-4f));
+    g = fma2(g, t, both(9.404923e-5f));
+    g = fma2(g, t, both(-0.10483512f));
+    g = fma2(g, t, both(-2.3022094f));
+    unpack2(mul2(x, g), a0, a1);
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(fminf(a0, 60.0f)));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(fminf(a1, 60.0f)));
+    unpack2(add2(pack2(e0, e1), both(1.0f)), d0, d1);
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d0 * d1));
-    unpack2(mul2(mul2(az, az), both(-1.4426950408889634f)), a0, a1);
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e0) : "f"(a0));
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e1) : "f"(a1));
-    const f32x2 t = pack2(r * d1, r * d0);
-    f32x2 pl = fma2(both(-0.5f * 1.061405429f), t, both(0.5f * 1.453152027f));           // minus half the polynomial
-    pl = fma2(pl, t, both(-0.5f * 1.421413741f));
-    pl = fma2(pl, t, both(0.5f * 0.284496736f));
-    pl = fma2(pl, t, both(-0.5f * 0.254829592f));
-    const f32x2 half_erf = fma2(mul2(pl, t), pack2(e0, e1), both(0.5f));                // of |z|
-    return mul2(x, add2(both(0.5f), (half_erf & 0x7fffffff7fffffffull) | (x & 0x8000000080000000ull)));
+    return mul2(x, pack2(r * d1, r * d0));
+}
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap *m, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];"
+                 ::"l"(m), "r"(src), "r"(c0), "r"(c1) : "memory");
 }
 enum { kNothing = 0, kGelu = 1, kAnything = 2 };                       // as in linear.cu
 
 template <int BN, int EPI>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
-linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ Fp8Params p)
+linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_y,
+                  const __grid_constant__ Fp8Params p)
 {
     constexpr int kAcc = 512 / BN < kMaxAcc ? 512 / BN : kMaxAcc;      // accumulators in turn
     constexpr int kCols = BN / 2;                                      // columns of a sum warp
@@ -129,7 +138,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
     __shared__ int stop;                                               // the stages that were sent for before the CTA gave up
 
     const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t sA = smem_base, sB = sA + kStages * kABytes, bars = sB + kStages * kBBytes;
+    const uint32_t sA = smem_base, sB = sA + kStages * kABytes, sBufs = sB + kStages * kBBytes, bars = sBufs + kSumWarps * kStageBytes;
     const uint32_t bar_full = bars, bar_empty = bars + 8 * kStages, bar_acc_full = bars + 16 * kStages,
                    bar_acc_empty = bar_acc_full + 8 * kMaxAcc, bar_end = bar_acc_empty + 8 * kMaxAcc;
 
@@ -150,7 +159,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         for (int a = 0; a < kMaxAcc; ++a) { mbar_init(bar_acc_full + 8 * a, 1); mbar_init(bar_acc_empty + 8 * a, 2 * kSumWarps); }
         fence_barrier_init();
     }
-    if (warp == kTmaWarp && elect_one()) { prefetch_tensormap(&tmap_w); prefetch_tensormap(&tmap_x); }
+    if (warp == kTmaWarp && elect_one()) { prefetch_tensormap(&tmap_w); prefetch_tensormap(&tmap_x); prefetch_tensormap(&tmap_y); }
     if (warp == kMmaWarp) {
         tmem_alloc_pair(smem_u32(&tmem_slot), kTmemCols);
         tmem_relinquish_pair();
@@ -168,36 +177,47 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
         const int part = warp >> 2, c0 = part * kCols;
         const int row = (int)rank * kRowsCta + (warp & 3) * 32 + lane;
         const uint32_t t_row = tmem + ((uint32_t)((warp & 3) * 32) << 16) + c0;
-        uint8_t *stage = smem_raw + (bars + kBarBytes - smem_u32(smem_raw)) + warp * kStageBytes;
-        const uint32_t s_stage = smem_u32(stage);
-        uint8_t *vectors = smem_raw + (bars + kBarBytes - smem_u32(smem_raw)) + kSumWarps * kStageBytes + warp * kVecBytes;
-        // A thread owns a row of the tile, and global memory is touched in 16-byte pieces: piece q of rows r0 + kStep j (see linear.cu; a bulk
-        // copy of each row's 64 bytes instead, by its own thread, took 1.4 times as long for 13106 x 1152 x 4608)
+        uint8_t *bufs = smem_raw + (sBufs - smem_u32(smem_raw)) + warp * kStageBytes;
+        const uint32_t s_bufs = smem_u32(bufs);
+        int buf = 0;                                                   // the one that is next
+        uint8_t *vectors = smem_raw + (bars + kBarBytes - smem_u32(smem_raw)) + warp * kVecBytes;
+        // A thread owns a row of the tile.  Where the rows of y lie one behind the other, a warp's 32 x 32 results go out of shared memory by TMA,
+        // under the next step: stores by the warp wait for the L2, which all SMs write to at the same time (13106 x 1152 x 4608: 84 us with
+        // them, 72 by TMA, 69 without any).  Rows at places of a list are stored by the warp, in 16-byte pieces: piece q of rows r0 + kStep j (see
+        // linear.cu; bulk copies of each row's 64 bytes took 1.4 times as long, TMA scatters of four rows were no faster: 90 us against 87).
         constexpr int kPieces = kChunk / 8, kStep = 32 / kPieces;
         const int q = lane % kPieces, r0 = lane / kPieces;
         auto swizzled = [](int r, int piece) { return r * (kChunk * 2) + ((piece ^ ((kPieces == 8 ? r : r >> 1) & (kPieces - 1))) << 4); };
+        // the buffer that is next has been read by the copy before the last
+        auto buf_free = [&] {
+            bulk_wait_read<1>();
+            __syncwarp();
+        };
         int acc = 0;
         uint32_t acc_phase = 0;
         // What a tile needs before its first block: the list's entries for its rows, the scales of the first blocks.  They are fetched in
         // front of the epilogue of the tile before (behind it, they were 1500 clocks of every tile).
-        int tok = 0, before = -1;
+        // (Loads that no branch guards, from places that exist: what stands for rows, columns and vectors that there are not is not used.  With
+        // branches the values were waited for here; 13106 x 1152 x 4608 with GELU 102 -> 98 us.)
+        int tok_next = 0, before_next = 0;
         uint4 vec_next = make_uint4(0, 0, 0, 0);                       // lanes 0-15: 8 columns of the bias each, 16-31: of the gate
-        int vec_batch = -1;                                            // the batch element that the gate belongs to
+        int vec_batch = 0;                                             // the batch element that the gate belongs to
         float xs_next[kAhead], ws_lane = 0.f;                          // scales of the row, kAhead blocks ahead (an L2 round trip is longer than a block)
+        const int *list = p.idx ? p.idx : reinterpret_cast<const int *>(p.x_scale);
+        const __nv_bfloat16 *vec_src = lane < 16 ? (p.bias ? p.bias : p.y) : (EPI == kAnything && p.gate ? p.gate : p.y);
+        const bool vec_gate = EPI == kAnything && p.gate && lane >= 16;
         auto fetch = [&](int tile) {
-            const int tm = tile / tiles_n, n0 = (tile - tm * tiles_n) * BN + c0;
-            const long long grow = (long long)tm * kTileRows + row;
-            const bool in_range = tile < total_tiles && grow < total_rows;
-            const int r = in_range ? (int)((unsigned)grow % (unsigned)p.M) : 0;
-            tok = in_range && p.idx ? __ldcg(p.idx + grow) : r;
-            before = in_range && p.idx && r > 0 ? __ldcg(p.idx + grow - 1) : -1;
+            const int there = tile < total_tiles ? tile : pair;
+            const int tm = there / tiles_n, n0 = (there - tm * tiles_n) * BN + c0;
+            const long long first = (long long)tm * kTileRows + (int)rank * kRowsCta + (warp & 3) * 32, grow = min(first + lane, total_rows - 1);
+            tok_next = __ldcg(list + grow);
+            before_next = __ldcg(list + (grow > 0 ? grow - 1 : 0));
 #pragma unroll
-            for (int u = 0; u < kAhead; ++u) xs_next[u] = in_range && u < k_steps ? __ldcg(p.x_scale + (long long)u * total_rows + grow) : 0.f;
-            ws_lane = tile < total_tiles && lane < k_steps ? __ldcg(p.w_scale + (long long)(n0 < p.N_out ? n0 / 128 : 0) * k_steps + lane) : 0.f;
-            vec_batch = __shfl_sync(0xffffffffu, in_range ? (int)((unsigned)grow / (unsigned)p.M) : 0, 0);
-            const __nv_bfloat16 *src = lane < 16 ? p.bias : EPI == kAnything && p.gate ? p.gate + (long long)vec_batch * p.N_out : nullptr;
+            for (int u = 0; u < kAhead; ++u) xs_next[u] = __ldcg(p.x_scale + (long long)min(u, k_steps - 1) * total_rows + grow);
+            ws_lane = __ldcg(p.w_scale + (long long)(n0 < p.N_out ? n0 / 128 : 0) * k_steps + min(lane, k_steps - 1));
+            if (EPI == kAnything) vec_batch = (unsigned)min(first, total_rows - 1) / (unsigned)p.M;
             const int col = n0 + (lane & 15) * 8;
-            vec_next = src && tile < total_tiles && (lane & 15) * 8 < kCols && col < p.N_out ? ld_cached(reinterpret_cast<const uint4 *>(src + col)) : make_uint4(0, 0, 0, 0);
+            vec_next = ld_cached(reinterpret_cast<const uint4 *>(vec_src + (vec_gate ? (long long)vec_batch * p.N_out : 0) + (col < p.N_out ? col : 0)));
         };
         fetch(pair);
         for (int tile = pair; tile < total_tiles; tile += n_pairs) {
@@ -206,6 +226,8 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
             const bool in_range = grow < total_rows;
             // the row of a [B, N, *] tensor; -1: past the end, an entry out of range or one that does not exceed its predecessor
             const int batch = in_range ? (int)((unsigned)grow / (unsigned)p.M) : 0;
+            const int place = in_range ? (int)grow - batch * p.M : 0;       // of the row in its list
+            const int tok = p.idx ? tok_next : place, before = p.idx && place > 0 ? before_next : -1;
             const bool bad = in_range && ((unsigned)tok >= (unsigned)p.N || before >= tok);
             const long long full_row = in_range && !bad ? (long long)batch * p.N + tok : -1;
             if (bad && tn == 0 && part == 0) atomicExch(p.err_word, kErrBadIndex);
@@ -219,10 +241,11 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                 return rrow >= 0 && col < p.N_out ? p.residual + (long long)rrow * p.N_out + col : nullptr;
             };
             if (EPI == kAnything && p.residual) {
+                buf_free();
 #pragma unroll
                 for (int j = 0; j < kPieces; ++j) {
                     const __nv_bfloat16 *src = residual_at(j, n0 + q * 8);
-                    cp_async_16(s_stage + swizzled(r0 + kStep * j, q), src ? src : p.residual, src != nullptr);
+                    cp_async_16(s_bufs + buf * kBufBytes + swizzled(r0 + kStep * j, q), src ? src : p.residual, src != nullptr);
                 }
             }
             const float *xs = p.x_scale + (in_range ? grow : 0), *ws = p.w_scale + (long long)(n0 < p.N_out ? n0 / 128 : 0) * k_steps;
@@ -259,6 +282,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
             }
             if (tile + n_pairs >= total_tiles) grid_launch_dependents();       // the last epilogue of this CTA
             fetch(tile + n_pairs);
+            const bool whole = __all_sync(0xffffffffu, p.whole && !bad && !abort_flag);
             int out_row[kPieces];                                           // rows r0 + kStep j of y
 #pragma unroll
             for (int j = 0; j < kPieces; ++j)
@@ -267,6 +291,8 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
 #pragma unroll
             for (int c = 0; c < kChunks; ++c) {
                 const int col0 = n0 + c * kChunk, colq = col0 + q * 8;      // this chunk's columns, the 8 that this lane moves
+                uint8_t *stage = bufs + buf * kBufBytes;
+                if (!(EPI == kAnything && p.residual) || c > 0) buf_free();
                 if (EPI == kAnything && p.residual) {
                     if (c == 0) asm volatile("cp.async.wait_all;" ::: "memory");
                     else {
@@ -301,7 +327,7 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                 }
                 if (EPI == kGelu || (EPI == kAnything && p.gelu)) {
 #pragma unroll
-                    for (int i = 0; i < kChunk / 2; ++i) f[i] = gelu2_one_reciprocal(f[i]);
+                    for (int i = 0; i < kChunk / 2; ++i) f[i] = gelu2_odds(f[i]);
                 }
                 if (EPI == kAnything && gate) {
 #pragma unroll
@@ -335,15 +361,24 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap tmap_w, const __grid_const
                     }
                     *mine = make_uint4(w[0], w[1], w[2], w[3]);
                 }
-                __syncwarp();
+                if (whole) {
+                    fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && col0 < p.N_out && grow < total_rows) tma_store_2d(&tmap_y, s_bufs + buf * kBufBytes, col0, (int)grow);
+                } else {
+                    __syncwarp();
 #pragma unroll
-                for (int j = 0; j < kPieces; ++j) {
-                    const uint4 t = *reinterpret_cast<const uint4 *>(stage + swizzled(r0 + kStep * j, q));
-                    if (out_row[j] >= 0 && colq < p.N_out) *reinterpret_cast<uint4 *>(p.y + (long long)out_row[j] * p.N_out + colq) = t;
+                    for (int j = 0; j < kPieces; ++j) {
+                        const uint4 t = *reinterpret_cast<const uint4 *>(stage + swizzled(r0 + kStep * j, q));
+                        if (out_row[j] >= 0 && colq < p.N_out) *reinterpret_cast<uint4 *>(p.y + (long long)out_row[j] * p.N_out + colq) = t;
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
+                bulk_commit();                           // (a group for every step, so that buf_free can count them)
+                buf ^= 1;
             }
         }
+        bulk_wait<0>();
     } else if (warp == kTmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegsOther));
         // ------------------------------------------------ TMA producer (the bytes of both CTAs are counted on the even one's barrier)
@@ -432,18 +467,35 @@ int32_t make_byte_map(CUtensorMap *map, const void *base, long long rows, int K,
     return ASTRAEA_OK;
 }
 
+// y as a matrix of rows one behind the other, by boxes of 32 columns x 32 rows; what lies outside is not written
+int32_t make_y_map(CUtensorMap *map, void *base, long long rows, int N_out)
+{
+    const EncodeTiledFn enc = reinterpret_cast<EncodeTiledFn>(tensor_map_encoder());
+    cuuint64_t dims[2] = {(cuuint64_t)N_out, (cuuint64_t)rows};
+    cuuint64_t strides[1] = {(cuuint64_t)N_out * 2};
+    cuuint32_t box[2] = {32, 32};
+    cuuint32_t estr[2] = {1, 1};
+    CUresult r = enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr,
+                     CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(ASTRAEA_ERR_INVALID_ARG, "astraea_gathered_linear_fp8: tensor map of y rejected (CUresult %d)", (int)r);
+    return ASTRAEA_OK;
+}
+
 template <int BN, int EPI>
 int32_t launch_tiles(const Fp8Params &p, const void *xq, const void *wq, int pairs, cudaStream_t stream)
 {
     CUtensorMap mw, mx;
     int32_t rc = make_byte_map(&mw, wq, p.N_out, p.K, BN / 2, "wq");
     if (rc == ASTRAEA_OK) rc = make_byte_map(&mx, xq, (long long)p.B * p.M, p.K, kRowsCta, "xq");
+    CUtensorMap my = mx;                          // (not used for rows that are not one behind the other)
+    if (rc == ASTRAEA_OK && p.whole) rc = make_y_map(&my, p.y, (long long)p.B * p.M, p.N_out);
     if (rc != ASTRAEA_OK) return rc;
     static PerDeviceOnce attrs;                   // the attribute is per device
     if (attrs.run([] { return cudaFuncSetAttribute(linear_fp8_kernel<BN, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes); }) != cudaSuccess)
         return check_launch("astraea_gathered_linear_fp8 (shared memory attribute)");
     const long long tiles = (((long long)p.B * p.M + kTileRows - 1) / kTileRows) * ((p.N_out + BN - 1) / BN);
-    launch_overlapped(linear_fp8_kernel<BN, EPI>, 2 * (int)(tiles < pairs ? tiles : pairs), kThreads, kSmemBytes, stream, mw, mx, p);
+    launch_overlapped(linear_fp8_kernel<BN, EPI>, 2 * (int)(tiles < pairs ? tiles : pairs), kThreads, kSmemBytes, stream, mw, mx, my, p);
     return check_launch("astraea_gathered_linear_fp8");
 }
 
@@ -472,6 +524,7 @@ int32_t launch_gathered_linear_fp8(const void *xq, const float *x_scale, const i
     p.compact = (flags & ASTRAEA_LINEAR_COMPACT_OUT) ? 1 : 0;
     p.res_compact = (flags & ASTRAEA_LINEAR_COMPACT_RES) ? 1 : 0;
     p.gelu = (flags & ASTRAEA_LINEAR_GELU) ? 1 : 0;
+    p.whole = !idx || p.compact ? 1 : 0;
     p.err_word = err_word;
     const int pairs = sm_count() / 2 > 0 ? sm_count() / 2 : 1;
     const long long tiles_m = ((long long)B * p.M + kTileRows - 1) / kTileRows;

@@ -229,3 +229,51 @@ def test_a_row_of_nan_stays_alone_and_runs_repeat(R):
     assert bool(again[0, 17].isnan().all()) and not bool(again[0, 44].isfinite().any())
     others = [r for r in range(R) if r not in (17, 44)]
     assert torch.equal(again[0, others], y[0, others])
+
+
+@pytest.mark.parametrize("N_out", [40, 264, 2056])
+@pytest.mark.parametrize("residual", [False, True])
+def test_bad_entries_among_compact_rows(N_out, residual):
+    """Compact rows go out 32 at a time, unless one of them is not to be written."""
+    g = torch.Generator("cuda").manual_seed(N_out)
+    B, N, M, K = 2, 900, 700, 384
+    xq, xs, wq, ws = operands(g, B * M, N_out, K)
+    idx = lists(g, B, N, M)
+    bad = {(0, 5): N, (0, 40): -1, (1, 699): 1 << 20, (1, 0): N + 3}
+    for (b, r), v in bad.items():
+        idx[b, r] = v
+    idx[0, 300] = idx[0, 299]                                       # does not exceed its predecessor
+    skipped = torch.zeros(B, M, dtype=torch.bool, device="cuda")
+    for b, r in list(bad) + [(0, 300)]:
+        skipped[b, r] = True
+    # the entry behind one that is too large does not exceed it either; the one behind -1 does
+    for b, r in ((0, 5), (1, 0)):
+        skipped[b, r + 1] = True
+    before = torch.randn(B, M, N_out, device="cuda", generator=g).bfloat16()
+    y = Guarded((B, M, N_out), torch.bfloat16, before)
+    work = A.new_workspace(A.OP_GATHERED_LINEAR_FP8, B, 0, N, M, K)
+    flags = A.LINEAR_COMPACT_OUT | (A.LINEAR_COMPACT_RES if residual else 0)
+    A.astraea_gathered_linear_fp8(xq, xs, idx, M, wq, ws, None, y.t if residual else None, None, y.t, B, N, K, N_out, flags=flags, workspace=work)
+    with pytest.raises(A.AstraeaError):
+        A.astraea_poll_error(work)
+    want, mass = product(xq, xs, wq, ws, N_out)
+    want, mass = want.unflatten(0, (B, M)), mass.unflatten(0, (B, M))
+    if residual:                                                    # in place
+        want, mass = want + before.double(), mass + before.double().abs() * 2.0 ** -6
+    close(y.t[~skipped], want[~skipped], mass[~skipped], K)
+    assert torch.equal(y.t[skipped], before[skipped])
+    y.check()
+
+
+@pytest.mark.parametrize("B,N,K,N_out", [(1, 4097, 256, 1160), (3, 700, 1152, 520), (1, 20000, 128, 264)])
+def test_all_rows_in_place_over_many_tiles(B, N, K, N_out):
+    g = torch.Generator("cuda").manual_seed(N)
+    xq, xs, wq, ws = operands(g, B * N, N_out, K)
+    before = torch.randn(B, N, N_out, device="cuda", generator=g).bfloat16()
+    y = Guarded((B, N, N_out), torch.bfloat16, before)
+    work = A.new_workspace(A.OP_GATHERED_LINEAR_FP8, B, 0, N, N, K)
+    A.astraea_gathered_linear_fp8(xq, xs, None, 0, wq, ws, None, y.t, None, y.t, B, N, K, N_out, workspace=work)
+    A.astraea_poll_error(work)
+    want, mass = product(xq, xs, wq, ws, N_out)
+    close(y.t.flatten(0, 1), want + before.double().flatten(0, 1), mass + before.double().flatten(0, 1).abs() * 2.0 ** -6, K)
+    y.check()
