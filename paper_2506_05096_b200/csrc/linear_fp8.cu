@@ -35,7 +35,7 @@ constexpr int kTileRows = 256, kRowsCta = kTileRows / 2, kBK = 128;    // bytes 
 constexpr int kSumWarps = 8;
 constexpr int kTmaWarp = kSumWarps, kMmaWarp = kTmaWarp + 1;
 constexpr int kThreads = (kSumWarps + 4) * 32;
-constexpr int kStages = 5;
+constexpr int kStages = 5;                                              // (six are no faster)
 constexpr int kABytes = kRowsCta * kBK, kBBytes = 128 * kBK;           // (B: half of at most 256 columns)
 constexpr int kBufBytes = 32 * 64;                                     // 32 rows x 32 bf16 columns on their way to / from global memory
 constexpr int kStageBytes = 2 * kBufBytes;                             // per sum warp: two of them in turn
