@@ -4,9 +4,9 @@
 // so that the largest value of a block takes the largest code (448) and the scales of all-zero blocks stay normal numbers.
 //
 // HBM-bound: two bytes in and one out for every value.  A warp takes a row; a block of 128 channels is 16 lanes with 16 bytes each, whose
-// largest magnitude goes round by four shuffles.  Four pairs of blocks are in flight per warp.  The quotient is x * (1 / scale) and one
-// residual step, which is the correctly rounded quotient for all but a few operands; a rounding of its own before the one to e4m3 would
-// decide the many exact ties that bf16 values have (a plain product moves 1 in 2000 codes of normal values by one).
+// largest magnitude goes round by four shuffles.  Four pairs of blocks are in flight per warp.  The quotient is x times both parts of 1 / scale,
+// which is the correctly rounded quotient for all but a few operands; a rounding of its own before the one to e4m3 would decide the many exact
+// ties that bf16 values have (a plain product moves 1 in 2000 codes of normal values by one).
 #include "common.cuh"
 
 namespace astraea {
@@ -26,8 +26,8 @@ __device__ __forceinline__ uint32_t largest(const uint4 &v) { return larger(larg
 // of both halves, as fp32
 __device__ __forceinline__ float magnitude(uint32_t m) { return fmaxf(fabsf(__uint_as_float(m << 16)), fabsf(__uint_as_float(m & 0xffff0000u))); }
 
-// Quotients by the reciprocal and one residual step: q = a r, q + (a - q b) r.
-struct BlockScale { float scale, inv, minus; };
+// The scale by a product and a residual step; 1 / scale as the sum of two numbers.
+struct BlockScale { float scale, inv, low; };
 __device__ __forceinline__ BlockScale scale_of(float amax) {
     BlockScale s;
     const float a = fmaxf(amax, kLeastAmax), q = a * (1.0f / kE4M3Max);
@@ -35,21 +35,20 @@ __device__ __forceinline__ BlockScale scale_of(float amax) {
     float r;
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s.scale));
     s.inv = fmaf(fmaf(-s.scale, r, 1.0f), r, r);
-    s.minus = -s.scale;
-    // an infinity in the block: 0 for what is finite, NaN for what is not, and no residual
-    if (a == INFINITY) { s.scale = a; s.inv = 0.f; s.minus = 0.f; }
+    s.low = fmaf(-s.scale, s.inv, 1.0f) * s.inv;
+    // an infinity in the block: 0 for what is finite, NaN for what is not
+    if (a == INFINITY) { s.scale = a; s.inv = 0.f; s.low = 0.f; }
     return s;
 }
 // eight values as e4m3
 __device__ __forceinline__ uint2 encode8(const uint4 &v, const BlockScale &s) {
     f32x2 x[4];
     unpack8(v, x);
-    const f32x2 inv = pack2(s.inv, s.inv), minus = pack2(s.minus, s.minus);
+    const f32x2 inv = pack2(s.inv, s.inv), low = pack2(s.low, s.low);
     uint32_t out[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        f32x2 q = mul2(x[i], inv);
-        q = fma2(fma2(q, minus, x[i]), inv, q);
+        const f32x2 q = fma2(x[i], inv, mul2(x[i], low));
         float lo, hi;
         unpack2(q, lo, hi);
         uint16_t c;
