@@ -9,7 +9,10 @@
 // head (16 bytes each; three times 8 bytes at head_dim 72, whose halves are 72 bytes), so that both ways of pairing channels, (2p, 2p + 1)
 // and (p, p + d/2), stay inside a lane and only the sums of the norm go round: over 4, 3 or 8 lanes.  The rows come through shared memory by
 // cp.async, one or two rounds of heads ahead, so that the loads of the next token run under the arithmetic of this one and cost no registers
-// (with loads into registers 71280 query and 118800 key rows of 24 x 128 took 412 us, now 385 = 6.2 TB/s).
+// (with loads into registers 71280 query and 118800 key rows of 24 x 128 took 412 us, now 383 = 6.3 TB/s).  Weights, biases and angles are
+// read from shared memory where they are used: at head_dim 72 they were 72 of 154 registers, and there is latency to hide (us with them in
+// registers / now: 13106 query and 32768 key rows of 16 x 72, layer norm 70 / 60, RMS norm 67 / 50; 80000 rows of 8 x 128 75 / 72; five blocks a SM,
+// with spills, 78, 58 and 75).
 // fp32 arithmetic, one rounding to bf16 at the end.
 #include <initializer_list>
 
@@ -59,6 +62,10 @@ __device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
 }
 
 // one access to a head: 16 or 8 bytes
+template <int U> __device__ __forceinline__ void load_shared(const void *p, uint32_t *r) {
+    if constexpr (U == 8) { const uint4 v = *reinterpret_cast<const uint4 *>(p); r[0] = v.x; r[1] = v.y; r[2] = v.z; r[3] = v.w; }
+    else { const uint2 v = *reinterpret_cast<const uint2 *>(p); r[0] = v.x; r[1] = v.y; }
+}
 template <int U> __device__ __forceinline__ void load_unit(const __nv_bfloat16 *p, uint32_t *r) {
     if constexpr (U == 8) {
         const uint4 v = ld_stream(reinterpret_cast<const uint4 *>(p));
@@ -100,7 +107,7 @@ template <int G> __device__ __forceinline__ float group_sum(float s, int lane) {
 
 // The weights and biases of a lane's channels.
 template <int DH, bool LAYER, int PAIRS, int BIAS>
-__device__ __forceinline__ void load_weights(const HeadTensor &t, int l, bool on, f32x2 (&w)[2][PAIRS], f32x2 (&bi)[2][BIAS])
+__device__ __forceinline__ void load_weights(const HeadTensor &t, int l, bool on, uint32_t (&w)[2][PAIRS], uint32_t (&bi)[2][BIAS])
 {
     using L = Lanes<DH>;
     constexpr int U = L::kUnit, G = L::kGroup;
@@ -116,14 +123,14 @@ __device__ __forceinline__ void load_weights(const HeadTensor &t, int l, bool on
                             if (LAYER && on && t.bias) load_unit<U>(t.bias + c, wb);
 #pragma unroll
                             for (int i = 0; i < U / 2; ++i) {
-                                w[s][j * (U / 2) + i] = widen(ww[i]);
-                                if (LAYER) bi[s][LAYER ? j * (U / 2) + i : 0] = widen(wb[i]);
+                                w[s][j * (U / 2) + i] = ww[i];
+                                if (LAYER) bi[s][LAYER ? j * (U / 2) + i : 0] = wb[i];
                             }
                         }
 }
 // A head: z is a lane's channels of its first and second half; co and si the cosines and sines of its channels (HALF) or of its pairs.
 template <int DH, bool LAYER, bool HALF, int PAIRS, int BIAS>
-__device__ __forceinline__ void norm_rotate(f32x2 (&z)[2][PAIRS], const f32x2 (&w)[2][PAIRS], const f32x2 (&bi)[2][BIAS], const float (&co)[2 * PAIRS],
+__device__ __forceinline__ void norm_rotate(f32x2 (&z)[2][PAIRS], const uint32_t (&w)[2][PAIRS], const uint32_t (&bi)[2][BIAS], const float (&co)[2 * PAIRS],
                                             const float (&si)[2 * PAIRS], float eps, int lane)
 {
     constexpr int G = Lanes<DH>::kGroup, kPairs = PAIRS;
@@ -149,7 +156,7 @@ __device__ __forceinline__ void norm_rotate(f32x2 (&z)[2][PAIRS], const f32x2 (&
 #pragma unroll
                         for (int i = 0; i < kPairs; ++i) {
                             z[s][i] = mul2(z[s][i], rstd);
-                            z[s][i] = LAYER ? fma2(z[s][i], w[s][i], bi[s][LAYER ? i : 0]) : mul2(z[s][i], w[s][i]);
+                            z[s][i] = LAYER ? fma2(z[s][i], widen(w[s][i]), widen(bi[s][LAYER ? i : 0])) : mul2(z[s][i], widen(w[s][i]));
                         }
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) {
@@ -167,7 +174,7 @@ __device__ __forceinline__ void norm_rotate(f32x2 (&z)[2][PAIRS], const f32x2 (&
 
 // LAYER: layer norm with a bias (RMS norm without one otherwise); HALF: channels are paired (p, p + DH/2) and not (2p, 2p + 1)
 template <int DH, bool LAYER, bool HALF>
-__global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_norm_kernel(const __grid_constant__ HeadNormParams p)
+__global__ void __launch_bounds__(kWarps * 32, 4) head_norm_kernel(const __grid_constant__ HeadNormParams p)
 {
     using L = Lanes<DH>;
     constexpr int U = L::kUnit, G = L::kGroup, kPairs = L::kUnits * U / 2;      // (f32x2 pairs of a half)
@@ -176,6 +183,15 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
     const bool on = sub < L::kHeads;
     grid_launch_dependents();
     grid_dependency_wait();
+    // weights and biases, ones and zeros where there are none
+    __shared__ __align__(16) uint16_t weights[2][2 * DH];
+    for (int i = threadIdx.x; i < 4 * DH; i += kWarps * 32) {
+        const HeadTensor &t = p.t[i / (2 * DH)];
+        const int c = i % (2 * DH);
+        const __nv_bfloat16 *src = c < DH ? t.weight : t.bias;
+        weights[i / (2 * DH)][c] = src ? __ldcg(reinterpret_cast<const uint16_t *>(src) + c % DH) : c < DH ? 0x3F80 : 0;
+    }
+    __syncthreads();
     // A unit is one token's heads of one tensor, or a share of them; it is gone through in rounds.  The list's entries are fetched a unit ahead
     // of the copies.
     struct Unit { int which, part, b, r, tok, before, h0, h1; };   // heads h0 .. h1 - 1; none behind the last unit
@@ -209,16 +225,13 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
                 const int c = lane + 32 * i, head = c / R::kHeadVecs;
                 if (c < R::kVecs && head < left) copy_async(to + c * 16, src + head * t.x_sh + (c - head * R::kHeadVecs) * 8);
             }
-            if (h0 == n.h0 && n.tok < p.n_rot && lane < 2 * R::kTableVecs) {
+            if (n.tok < p.n_rot && lane < 2 * R::kTableVecs) {
                 const float *table = lane < R::kTableVecs ? p.cos : p.sin;
                 copy_async(to + (R::kVecs + lane) * 16, table + (size_t)n.tok * (DH / 2) + (lane % R::kTableVecs) * 4);
             }
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    int held = -1;                                                 // tensor whose weights are held
-    f32x2 w[2][kPairs], bi[2][LAYER ? kPairs : 1];
-    float co[kPairs * 2], si[kPairs * 2];                          // HALF: of the lane's channels; else of the pairs of both of its halves
     const int stride = gridDim.x * kWarps;
     int u = blockIdx.x * kWarps + warp, slot = 0;
     Unit now = unit_at(u), ahead = unit_at(u + stride);
@@ -241,23 +254,8 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
         } else {
             const HeadTensor &t = p.t[now.which];
             const uint8_t *mine = rounds + slot * R::kBytes;
-            if (now.which != held) {
-                held = now.which;
-                load_weights<DH, LAYER>(t, l, on, w, bi);
-            }
-            if (hr == now.h0) {                                     // a new token's angles
-                const bool turned = on && now.tok < p.n_rot;
-                const float *pc = reinterpret_cast<const float *>(mine + R::kVecs * 16), *ps = pc + DH / 2;
-#pragma unroll
-                for (int j = 0; j < L::kUnits; ++j)
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const int c0 = (l + G * j) * U;             // first channel of the access, in its half
-                        const int from = HALF ? c0 + s * (U / 2) : s * (DH / 4) + c0 / 2, to = HALF ? j * U + s * (U / 2) : s * kPairs + j * (U / 2);
-#pragma unroll
-                        for (int i = 0; i < U / 2; ++i) { co[to + i] = turned ? pc[from + i] : 1.f; si[to + i] = turned ? ps[from + i] : 0.f; }
-                    }
-            }
+            const bool turned = on && now.tok < p.n_rot;
+            const float *pc = reinterpret_cast<const float *>(mine + R::kVecs * 16), *ps = pc + DH / 2;
             __nv_bfloat16 *dst = t.y + now.b * t.y_sb + (int64_t)(t.compact_out ? now.r : now.tok) * t.y_sn + l * U;
             const int hb = hr + sub, h1 = now.h1;
 #pragma unroll
@@ -269,10 +267,26 @@ __global__ void __launch_bounds__(kWarps * 32, LAYER && DH == 72 ? 3 : 4) head_n
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int j = 0; j < L::kUnits; ++j) {
-                        const uint8_t *at = mine + (k * L::kHeads + (on ? sub : 0)) * (DH * 2) + s * DH + (l + G * j) * (U * 2);
-                        uint32_t *to = &raw[s][j * (U / 2)];
-                        if constexpr (U == 8) { const uint4 v = *reinterpret_cast<const uint4 *>(at); to[0] = v.x; to[1] = v.y; to[2] = v.z; to[3] = v.w; }
-                        else { const uint2 v = *reinterpret_cast<const uint2 *>(at); to[0] = v.x; to[1] = v.y; }
+                        load_shared<U>(mine + (k * L::kHeads + (on ? sub : 0)) * (DH * 2) + s * DH + (l + G * j) * (U * 2), &raw[s][j * (U / 2)]);
+                    }
+                uint32_t w[2][kPairs], bi[2][LAYER ? kPairs : 1];
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int j = 0; j < L::kUnits; ++j) {
+                        const uint16_t *pw = weights[now.which] + s * (DH / 2) + (l + G * j) * U;
+                        load_shared<U>(pw, &w[s][j * (U / 2)]);
+                        if constexpr (LAYER) load_shared<U>(pw + DH, &bi[s][j * (U / 2)]);
+                    }
+                float co[kPairs * 2], si[kPairs * 2];              // HALF: of the lane's channels; else of the pairs of both of its halves
+#pragma unroll
+                for (int j = 0; j < L::kUnits; ++j)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int c0 = (l + G * j) * U;             // first channel of the access, in its half
+                        const int from = HALF ? c0 + s * (U / 2) : s * (DH / 4) + c0 / 2, to = HALF ? j * U + s * (U / 2) : s * kPairs + j * (U / 2);
+#pragma unroll
+                        for (int i = 0; i < U / 2; ++i) { co[to + i] = turned ? pc[from + i] : 1.f; si[to + i] = turned ? ps[from + i] : 0.f; }
                     }
                 f32x2 z[2][kPairs];
 #pragma unroll
@@ -306,7 +320,7 @@ __global__ void __launch_bounds__(kWarps * 32, 3) few_heads_kernel(const __grid_
     grid_dependency_wait();
     const HeadTensor &t = p.t[which];
     const long long rows = (long long)B * t.M * t.H;               // (token, head) pairs
-    f32x2 w[2][kPairs], bi[2][LAYER ? kPairs : 1];
+    uint32_t w[2][kPairs], bi[2][LAYER ? kPairs : 1];
     load_weights<DH, LAYER>(t, l, on, w, bi);
     const long long step = (long long)gridDim.x * kWarps * kSteps * L::kHeads;
     for (long long base = ((long long)blockIdx.x * kWarps + (threadIdx.x >> 5)) * kSteps * L::kHeads; base < rows; base += step) {
