@@ -198,3 +198,47 @@ def test_many_rows_and_another_stream():
     c, s = cos.double()[None, :, None], sin.double()[None, :, None]
     want = torch.stack([z[..., 0::2] * c - z[..., 1::2] * s, z[..., 0::2] * s + z[..., 1::2] * c], -1).flatten(-2)
     close(y, want, z, False)
+
+
+@pytest.mark.parametrize("d,H", [(64, 49), (72, 21), (72, 41), (128, 50)])
+@pytest.mark.parametrize("norm,rotation", [(A.NORM_RMS, A.ROTATE_HALF), (A.NORM_LAYER, A.ROTATE_INTERLEAVED)])
+def test_heads_that_take_several_rounds(d, H, norm, rotation):
+    test_listed_queries_and_all_keys_in_one_launch(d, H, norm, rotation)
+    # and in a launch that gives a warp more than one token, each with all its heads
+    g = torch.Generator("cuda").manual_seed(H)
+    B, N = 1, 5003
+    x = 3 * torch.randn(B, N, H, d, device="cuda", generator=g).bfloat16()
+    y = Guarded((B, N, H, d), torch.bfloat16)
+    w = torch.randn(d, device="cuda", generator=g).bfloat16()
+    cos, sin = table(N - 3, d, g)
+    st = A.bhnd_strides(N, H, d)
+    A.astraea_qk_norm_rotate([A.head_rows(x, st, y.t, st, H, weight=w)], cos, sin, N - 3, B, N, d, norm, rotation, EPS)
+    some = torch.cat([torch.arange(40), torch.arange(2500, 2540), torch.arange(N - 40, N)])
+    want, z = reference(x[:, some], some[None], N - 3, cos, sin, w, None, norm, rotation)
+    close(y.t[:, some], want, z, norm == A.NORM_LAYER)
+    y.check()
+
+
+@pytest.mark.parametrize("d", [64, 72, 128])
+@pytest.mark.parametrize("H,H_kv", [(1, 16), (16, 1), (1, 1)])
+@pytest.mark.parametrize("empty", [0, 1])
+def test_an_empty_list_beside_all_rows_in_place(d, H, H_kv, empty):
+    g = torch.Generator("cuda").manual_seed(d + H)
+    B, N, n_rot = 2, 5500, 5400
+    heads = (H, H_kv)
+    x = [3 * torch.randn(B, N, h, d, device="cuda", generator=g).bfloat16() for h in heads]
+    y = [Guarded((B, N, h, d), torch.bfloat16, v) for h, v in zip(heads, x)]
+    w = [torch.randn(d, device="cuda", generator=g).bfloat16() for _ in heads]
+    cos, sin = table(n_rot, d, g)
+    nothing = torch.zeros(B, 0, dtype=torch.int32, device="cuda")
+    rows = []
+    for i in (0, 1):
+        st = A.bhnd_strides(N, heads[i], d)
+        rows.append(A.head_rows(y[i].t, st, y[i].t, st, heads[i], nothing if i == empty else None, 0, w[i]))
+    A.astraea_qk_norm_rotate(rows, cos, sin, n_rot, B, N, d, A.NORM_RMS, A.ROTATE_HALF, EPS)
+    assert torch.equal(y[empty].t, x[empty])
+    full = 1 - empty
+    some = torch.cat([torch.arange(60), torch.arange(5380, 5420), torch.arange(N - 20, N)])
+    want, z = reference(x[full][:, some], some.expand(B, -1), n_rot, cos, sin, w[full], None, A.NORM_RMS, A.ROTATE_HALF)
+    close(y[full].t[:, some], want, z, False)
+    y[0].check(); y[1].check()
