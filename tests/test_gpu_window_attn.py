@@ -215,3 +215,31 @@ def test_split_by_keys_is_the_unsplit_launch_and_repeats(d):
     check(*split); check(*whole)
     assert torch.equal(split[0], again[0]) and torch.equal(split[1], again[1])
     assert (split[0].float() - whole[0].float()).abs().max() <= 2.0 ** -7 * whole[0].float().abs().max()
+
+
+@pytest.mark.parametrize("d", [64, 72, 128])
+def test_keys_shared_by_the_batch_and_offsets_past_32_bits(d):
+    g = torch.Generator("cuda").manual_seed(d)
+    B, N, M, H, H_kv, left, right = 2, 2100, 40, 4, 2, 150, 90
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()
+    q, k, v = rnd(B, N, H, d), rnd(1, N, H_kv, d).expand(B, -1, -1, -1), rnd(1, N, H_kv, d)
+    v[0, N - 30, 1, 3] = math.inf                                   # in the last windows
+    v = v.expand(B, -1, -1, -1)
+    idx = lists(g, B, N, M)
+    idx[:, -1] = N - 1
+    apart = 1 << 20                                                 # elements between two tokens: the last ones lie 2.2e9 elements in
+    room = torch.empty(N * apart, device="cuda", dtype=torch.bfloat16)
+    far_k = room.as_strided((N, H_kv, d), (apart, d, 1))
+    far_v = room.as_strided((N, H_kv, d), (apart, d, 1), 4 * 128)
+    far_k.copy_(k[0]); far_v.copy_(v[0])
+    out, lse = torch.zeros(B, M, H, d, device="cuda", dtype=torch.bfloat16), torch.zeros(B, H, M, device="cuda")
+    ws = A.new_workspace(A.OP_WINDOW_ATTN, B, H, N, M, d)
+    st = (0, d, apart)
+    A.astraea_window_attn(q, far_k, far_v, A.bhnd_strides(N, H, d), st, st, idx, M, out, lse, B, H, H_kv, N, d, 0, 0, left, right,
+                          flags=A.ATTN_COMPACT_OUT, workspace=ws)
+    A.astraea_poll_error(ws)
+    rows = torch.arange(B, device="cuda")[:, None]
+    want, want_lse = reference(q[rows, idx.long()], k, v, idx, N, 0, 0, left, right, None, 1 / math.sqrt(d))
+    odd = ~want.isfinite()
+    assert odd.any() and torch.equal(~out.isfinite(), odd)
+    check(torch.where(odd, 0.0, out.float()).bfloat16(), lse, torch.where(odd, 0.0, want), want_lse)
