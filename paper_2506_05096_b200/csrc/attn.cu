@@ -45,8 +45,6 @@
 // tcgen05.mma several times slower).  Every mbarrier wait is bounded; on a timeout the CTA raises
 // the error word, the remaining waits return at once, no further copy is sent for, and the CTA runs out; it leaves when
 // the copies and MMAs that were under way have ended.
-#include <limits.h>
-
 #include <mutex>
 #include <type_traits>
 
@@ -266,7 +264,7 @@ struct SoftmaxState {
 struct WindowState : SoftmaxState {
     const KeyList *keys;            // of the CTA (shared memory)
     int tile0;                      // its first key tile in that list
-    int lo, hi;                     // keys in reach of this thread's row
+    int lo, hi;                     // keys in reach of this thread's row (kNoRowLo, kNoRowHi: there is none)
     int n_first, last0;
     bool seen;                      // some key of the CTA's tiles is visible to the row
 };
@@ -430,7 +428,9 @@ __device__ __forceinline__ void softmax_step(StateOf<C> &st, int j, int g)
     pack_p<NS>(cur, pk);
     if constexpr (MODE == kSpeculate && !C::kOnes) {
         // rare: the reference is too low for this tile.  The CTA finishes the pass and redoes its work with exact maxima
-        if (__any_sync(0xffffffffu, !(tile_sum <= kTileSumLimit))) *st.redo_flag = 1;
+        bool counts = true;                           // (not of a row that does not exist)
+        if constexpr (C::kWindow) counts = st.lo != kNoRowLo;
+        if (__any_sync(0xffffffffu, counts && !(tile_sum <= kTileSumLimit))) *st.redo_flag = 1;
     }
     st.l_sum += tile_sum;
     store_p<NS>(t_s, pk);                         // over the first NS/2 columns of this S buffer
@@ -542,15 +542,14 @@ __device__ __forceinline__ void softmax_role(const ParamsOf<C> &p, const Bars &b
     if constexpr (C::kWindow) {
         st.keys = keys; st.tile0 = tile0;
         st.n_first = p.n_first; st.last0 = p.last0;
-        st.lo = tok - p.left; st.hi = tok + p.right;
+        st.lo = tok >= 0 ? tok - p.left : kNoRowLo; st.hi = tok >= 0 ? tok + p.right : kNoRowHi;
         st.seen = false;
     }
     // a pass over this warpgroup's key tiles
     auto run_pass = [&](auto mode, int g0) {
         constexpr int MODE = decltype(mode)::value;
         if constexpr (C::kWindow) {
-            const WholeTiles whole = whole_tiles(*keys, __reduce_max_sync(0xffffffffu, tok >= 0 ? st.lo : INT_MIN),
-                                                 __reduce_min_sync(0xffffffffu, tok >= 0 ? st.hi : INT_MAX), p.n_first, p.last0);
+            const WholeTiles whole = whole_tiles(*keys, __reduce_max_sync(0xffffffffu, st.lo), __reduce_min_sync(0xffffffffu, st.hi), p.n_first, p.last0);
             for (int j = par; j < n_tiles; j += kSplit) {
                 if (whole.has(tile0 + j)) softmax_step<C, MODE>(st, j, g0 + j);
                 else softmax_step<C, MODE, true>(st, j, g0 + j);

@@ -7,6 +7,8 @@
 // tiles whatever its place, and the tiles are numbered through.
 #pragma once
 
+#include <limits.h>
+
 constexpr int kKeyTile = 64;
 // A row's sum of exponentials against the speculative reference below which it is redone against its exact maximum
 constexpr float kLeastSum = 8.271806125530277e-25f;              // 2^-80
@@ -20,6 +22,10 @@ struct KeyList {
     __device__ __forceinline__ int key(int j) const { return j < b_tile ? kKeyTile * j : j < c_tile ? b0 + kKeyTile * (j - b_tile) : c0 + kKeyTile * (j - c_tile); }
     __device__ __forceinline__ int end(int j) const { return j < b_tile ? a1 : j < c_tile ? b1 : c1; }
 };
+
+// What a row of the CTA that does not exist (behind the last one, a bad entry of the list) reaches: neutral where a warp takes the largest lo and
+// the smallest hi of its rows.  It sees no key, and a warp of such rows takes no tile for whole.
+constexpr int kNoRowLo = INT_MIN, kNoRowHi = INT_MAX;
 
 struct GroupRow { int m, rest; };        // row m * group + rest of a key head's (query, head) pairs
 struct WindowParams : Params {
@@ -65,14 +71,15 @@ __device__ __forceinline__ KeyList list_keys(const WindowParams &p, int b, int f
 }
 
 // The tiles of which rows that all reach keys lo .. hi see every key: up to three runs of tile numbers (a tile that is seen whole only
-// because two reasons meet in it is not among them).
+// because two reasons meet in it is not among them).  None where there is no row (lo = kNoRowLo).
 struct WholeTiles {
     int first, w0, w_n, l0, l_n;         // tiles below `first`, w_n from w0 on, l_n from l0 on
     __device__ __forceinline__ bool has(int j) const { return j < first || (unsigned)(j - w0) < (unsigned)w_n || (unsigned)(j - l0) < (unsigned)l_n; }
 };
 __device__ __forceinline__ WholeTiles whole_tiles(const KeyList &k, int lo, int hi, int n_first, int last0)
 {
-    WholeTiles t;
+    WholeTiles t = {};
+    if (lo == kNoRowLo) return t;
     t.first = min(n_first, k.a1) / kKeyTile;
     auto run = [](int from, int to, int base, int tile, int &t0, int &n) {      // keys from .. to - 1 of a range
         const int a = (max(from - base, 0) + kKeyTile - 1) / kKeyTile, b = max(to - base, 0) / kKeyTile;
@@ -88,9 +95,10 @@ __device__ __forceinline__ uint64_t bits_between(int a, int b)
     a = max(a, 0); b = min(b, 64);
     return b > a ? (~0ull >> (64 - (b - a))) << a : 0ull;
 }
-// The keys of that tile that a row which reaches lo .. hi sees, a bit each.
+// The keys of that tile that a row which reaches lo .. hi sees, a bit each (none for a row that does not exist).
 __device__ __forceinline__ uint64_t visible_bits(int k0, int end, int lo, int hi, int n_first, int last0)
 {
+    if (lo == kNoRowLo) return 0ull;
     return (bits_between(0, n_first - k0) | bits_between(lo - k0, hi + 1 - k0) | bits_between(last0 - k0, 64)) & bits_between(0, end - k0);
 }
 template <int NS> __device__ __forceinline__ void hide(float (&s)[NS], uint64_t visible, float with)
