@@ -1726,7 +1726,7 @@ SplitPlan window_plan(const WindowArgs &a, int tm)
     const double whole = finish_time(units, groups, light_last, slots, 0, 1);
     double best = whole;
     for (int s = 2; s <= kMaxWindowSplit && s * 2 <= tiles; ++s) {
-        if ((long long)tail * s > kMaxSplitParts || split_bytes((long long)tail * s, a.a.d) > a.a.split_ws_bytes) break;
+        if ((long long)tail * s > kMaxSplitParts || split_bytes((long long)tail * s, a.a.d, unit_rows) > a.a.split_ws_bytes) break;
         const double t = finish_time(units, groups, light_last, slots, tail, s, 4.0 / (double)tiles);
         if (t < 0.97 * whole && t < best) { best = t; plan.units = tail; plan.split = s; }
     }

@@ -172,10 +172,11 @@ struct WindowArgs {
     const int32_t *kv_len;
 };
 int32_t launch_window_attn(const WindowArgs &w, cudaStream_t stream);
-// 256 bytes for the error word and room for the key shares of up to kMaxWindowSplit CTAs a unit (fp32 rows and LSEs of 256 rows each)
+// 256 bytes for the error word and room for the key shares of up to kMaxWindowSplit CTAs a unit (fp32 rows and LSEs of 256 rows each; small CTAs
+// have twice as many units of 128)
 constexpr int kMaxWindowSplit = 16;          // shares per unit: the heads of a single token are all that one (batch, key head) has
 constexpr int kMaxSplitParts = 2 * 148;      // shares per launch
-inline size_t split_bytes(long long parts, int d) { return (size_t)parts * 256 * ((size_t)d * 4 + 4) + 256; }
+inline size_t split_bytes(long long parts, int d, int unit_rows = 256) { return (size_t)parts * unit_rows * ((size_t)d * 4 + 4) + 256; }
 inline size_t window_workspace_bytes(int B, int H, int M, int d) {
     if (B <= 0 || H <= 0 || M <= 0 || d <= 0) return 256;
     const long long parts = (long long)B * H * ((M + 255ll) / 256) * kMaxWindowSplit;

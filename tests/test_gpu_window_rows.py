@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+from helpers import Guarded
 from paper_2506_05096_b200 import binding as A
 from test_gpu_window_attn import check, reference
 
@@ -63,3 +64,32 @@ def test_skipped_entries_hold_nothing_back(d):
     check(out[:, good], lse[:, :, good], want, want_lse)
     rest = skipped + [201]
     assert bool((out[:, rest] == 7).all()) and bool((lse[:, :, rest] == 7).all())
+
+
+@pytest.mark.parametrize("d", [64, 72])
+@pytest.mark.parametrize("M", [129, 200, 256])
+def test_the_workspace_asked_for_holds_every_share_of_small_ctas(d, M):
+    """A call of two units of 128 rows is shared out as far with the bytes of astraea_workspace_bytes as with any more, and stays inside them."""
+    g = torch.Generator("cuda").manual_seed(M + d)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g).bfloat16()
+    N = 9000
+    q, k, v = rnd(1, M, 1, d), rnd(1, N, 1, d), rnd(1, N, 1, d)
+    idx = (torch.arange(M, device="cuda", dtype=torch.int32)[None] * 35).contiguous()
+    asked = A.new_workspace(A.OP_WINDOW_ATTN, 1, 1, N, M, d).numel()
+    results = []
+    for size in (asked, asked + (64 << 20)):
+        ws = Guarded((size + 4096,), torch.uint8)                 # (a workspace begins at a multiple of 256 bytes)
+        skip = -ws.t.data_ptr() % 256
+        ws.t[skip:skip + size] = 0
+        behind = ws.t[skip + size:].clone()
+        out, lse = torch.zeros_like(q), torch.zeros(1, 1, M, device="cuda")
+        st = A.bhnd_strides(N, 1, d)
+        A.astraea_window_attn(q, k, v, A.bhnd_strides(M, 1, d), st, st, idx, M, out, lse, 1, 1, 1, N, d, 0, 0, N, N,
+                              flags=A.ATTN_COMPACT_Q | A.ATTN_COMPACT_OUT | A.ATTN_SMALL_CTAS, workspace=ws.t[skip:skip + size])
+        A.astraea_poll_error(ws.t[skip:skip + size])
+        ws.check()
+        assert torch.equal(ws.t[skip + size:], behind)
+        want, want_lse = reference(q, k, v, idx, N, 0, 0, N, N, None, 1 / math.sqrt(d))
+        check(out, lse, want, want_lse)
+        results.append((out, lse))
+    assert torch.equal(results[0][0], results[1][0]) and torch.equal(results[0][1], results[1][1])
