@@ -8,7 +8,7 @@
 // them in short launches), whose cosines and sines it reads once.  A lane owns the same channels of the first and of the second half of a
 // head (16 bytes each; three times 8 bytes at head_dim 72, whose halves are 72 bytes), so that both ways of pairing channels, (2p, 2p + 1)
 // and (p, p + d/2), stay inside a lane and only the sums of the norm go round: over 4, 3 or 8 lanes.  The rows come through shared memory by
-// cp.async, one or two rounds of heads ahead, so that the loads of the next token run under the arithmetic of this one and cost no registers
+// cp.async, a round of heads ahead, so that the loads of the next token run under the arithmetic of this one and cost no registers
 // (with loads into registers 71280 query and 118800 key rows of 24 x 128 took 412 us, now 383 = 6.3 TB/s).  Weights, biases and angles are
 // read from shared memory where they are used: at head_dim 72 they were 72 of 154 registers, and there is latency to hide (us with them in
 // registers / now: 13106 query and 32768 key rows of 16 x 72, layer norm 70 / 60, RMS norm 67 / 50; 80000 rows of 8 x 128 75 / 72; five blocks a SM,
@@ -22,6 +22,7 @@ namespace astraea {
 namespace {
 
 constexpr int kWarps = 4;                                          // per block
+constexpr int kBlocksSM = 4;                                       // blocks of head_norm_kernel on an SM: 128 registers a thread, 54 KB at head_dim 128
 
 struct HeadTensor {
     const __nv_bfloat16 *x;
@@ -174,7 +175,7 @@ __device__ __forceinline__ void norm_rotate(f32x2 (&z)[2][PAIRS], const uint32_t
 
 // LAYER: layer norm with a bias (RMS norm without one otherwise); HALF: channels are paired (p, p + DH/2) and not (2p, 2p + 1)
 template <int DH, bool LAYER, bool HALF>
-__global__ void __launch_bounds__(kWarps * 32, 4) head_norm_kernel(const __grid_constant__ HeadNormParams p)
+__global__ void __launch_bounds__(kWarps * 32, kBlocksSM) head_norm_kernel(const __grid_constant__ HeadNormParams p)
 {
     using L = Lanes<DH>;
     constexpr int U = L::kUnit, G = L::kGroup, kPairs = L::kUnits * U / 2;      // (f32x2 pairs of a half)
@@ -391,11 +392,13 @@ int32_t launch_dim(HeadNormParams &p, int n, int B, bool layer, bool half, cudaS
     if (alone[0]) { p.t[0] = p.t[1]; alone[0] = alone[1]; --n; }
     if (n == 2 && alone[1]) n = 1;
     if (n == 0 || (n == 1 && alone[0])) return ASTRAEA_OK;
-    // A token's heads go to one warp where that gives every SM its 32 warps, and are shared out in steps of a warp's heads where it does
-    // not: one token of 32 + 8 heads is then 10 warps and not 2.
+    // A token's heads go to one warp where that gives every SM the warps that it holds, and are shared out in steps of a warp's heads where it
+    // does not: one token of 32 + 8 heads is then 10 warps and not 2.  More shares than there is room for wait, and each reads its token's
+    // angles again (us for 600 / 1500 / 2300 rows of 24 x 128 with twice as many 5.9 / 7.2 / 8.2, now 4.3 / 5.9 / 6.2; of 16 x 72, layer norm, 3.8 /
+    // 6.3 / 7.6 and 3.8 / 5.1 / 5.3; of 32 x 128 5.7 / 8.3 / 9.7 and 4.9 / 8.4 / 8.6).
     long long all_rows = 0;
     for (int i = 0; i < n; ++i) all_rows += (long long)B * p.t[i].M;
-    const long long slots = (long long)sm_count() * 32;
+    const long long slots = (long long)sm_count() * (kWarps * kBlocksSM);
     long long units[2] = {0, 0};
     for (int i = 0; i < n; ++i) {
         HeadTensor &t = p.t[i];
@@ -416,6 +419,7 @@ int32_t launch_dim(HeadNormParams &p, int n, int B, bool layer, bool half, cudaS
     auto kernel = layer ? (half ? head_norm_kernel<DH, true, true> : head_norm_kernel<DH, true, false>)
                         : (half ? head_norm_kernel<DH, false, true> : head_norm_kernel<DH, false, false>);
     constexpr int kSmem = kWarps * 2 * Round<DH>::kBytes;           // 52 KB at head_dim 128
+    static_assert(kBlocksSM * (kSmem + 8 * DH + 1024) <= 228 * 1024, "shared memory of the blocks of an SM");
     static PerDeviceOnce attrs;                   // the attribute is per device (all four kernels of the width at once)
     if (attrs.run([] {
             cudaError_t e = cudaSuccess;
