@@ -1168,6 +1168,7 @@ sparse_attn_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_cons
     } else if constexpr (C::kWindow) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::kRegsOther));
         // ------------------------------------------------ looks at the values of a stage before the MMAs (see clear_odd)
+        static_assert(4 * kCleanLoads + 20 <= C::kRegsOther, "the loads in flight, an address, a counter, the largest magnitude and the loop around them");
         const int lane = tid & 31;
         const WholeTiles whole = whole_tiles(key_list, key_list.all_lo, key_list.all_hi, p.n_first, p.last0);
         auto look_pass = [&](int gv0) {

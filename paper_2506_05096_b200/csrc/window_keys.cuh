@@ -150,11 +150,14 @@ __device__ __forceinline__ void largest(uint32_t &m, const uint4 &v)
 }
 // A tile of values in shared memory (a row is 128 bytes in each of the chunks of CHUNK_BYTES and 32 in what is left of LOAD_BYTES behind
 // them; the swizzle keeps a row's bytes in its row) by one warp: rows from `rows` on and elements that are not finite become zero.  True if
-// there were such elements in the rows before.  Read with eight loads in flight, and written only where there is something to clear.
+// there were such elements in the rows before.  Written only where there is something to clear.  Two loads are in flight: the warp has 32
+// registers, and a load takes four of them (us with one / two / four / eight: 4613 of 17776 queries, 2048 keys either way, 24 heads of 64 216 / 216 /
+// 223 / 220; 1000 of them, 300 keys either way 63 / 63 / 70 / 67, with heads of 128 92 / 92 / 92 / 94).
+constexpr int kCleanLoads = 2;
 template <int CHUNK_BYTES, int CHUNKS, int LOAD_BYTES>
 __device__ __forceinline__ bool clean_values(uint4 *v, int rows, int lane)
 {
-    constexpr int kVecs = LOAD_BYTES / 16, kMain = CHUNKS * CHUNK_BYTES / 16, kRound = kVecs % 256 == 0 ? 8 : kVecs % 160 == 0 ? 5 : 4;
+    constexpr int kVecs = LOAD_BYTES / 16, kMain = CHUNKS * CHUNK_BYTES / 16, kRound = kCleanLoads;
     static_assert(kVecs % (32 * kRound) == 0, "whole rounds");
     auto row_of = [](int i) { return i < kMain ? i / 8 % kKeyTile : (i - kMain) / 2; };
     bool odd = false;
