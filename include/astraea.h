@@ -400,6 +400,7 @@ int32_t astraea_qk_norm_rotate(const astraea_head_rows *rows, int n, const float
 /*
  * Operands of a linear layer in 8 bits: e4m3 codes with a scale for each 128 channels,
  *     scale = max(largest magnitude of the block, 2^-100) / 448,     code = x / scale, rounded to e4m3 (ties to even).
+ * The scale and the quotient by it are rounded to fp32 first, which may decide where the exact quotient is a tie or next to one.
  * astraea_quantize_fp8: the listed rows of x, a block being 128 channels of a row.
  *   x       : bf16 [B, N, K] (ASTRAEA_LINEAR_COMPACT_IN: [B, M, K])
  *   idx     : int32 [B, M] strictly ascending in [0, N); NULL => all N rows (M ignored)

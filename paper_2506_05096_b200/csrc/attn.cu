@@ -75,7 +75,8 @@ constexpr uint32_t kGaveUpLse = 0xffc0dead;
 // DH: head_dim.  TM: 128-row query tiles per CTA.  Two share every K/V tile in shared memory and run one CTA per SM;
 // one (head_dim 64 / 72 only) lets two CTAs share an SM, which costs ~5 % of throughput per SM but halves the
 // granularity of the schedule: launches of only a few rounds of CTAs are faster with it.
-// WIN: attention over a window of keys (window_keys.cuh).
+// WIN: attention over a window of keys (window_keys.cuh); what a row's reach and the key list add to the softmax warps spills 16 bytes a thread in
+// large CTAs and 24 in small ones (the plain form in small CTAs at head_dim 72 spills 24, too).
 template <int DH, int TM, bool WIN = false> struct Cfg {
     static constexpr bool kWindow = WIN;
     static_assert(TM == 2 || DH != 128, "head_dim 128 needs the whole SM");

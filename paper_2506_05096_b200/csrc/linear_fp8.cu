@@ -14,8 +14,9 @@
 // accumulator (512 of MMAs, 234 from their end to the warps that wait for it, the reads, 143 for the arrival at the other CTA) and the
 // issue slots of the warps that do all this, so: eight warps of 128 columns and not sixteen of 64 (the loop around the FMAs is paid half
 // as often), loads of 64 columns, the accumulator released when the last load has landed and before its FMAs, descriptors and phases
-// counted on, not computed, scales fetched four blocks ahead.  16384 x 6144 x 6144: 588 -> 413 us on zeros (clocks at their maximum), 503 us =
-// 2.46 PFLOP/s on random codes, where the power cap takes the clocks to 1.6 GHz.  (128-column tiles by two sets of warps in turn, whose epilogues
+// counted on, not computed, scales fetched four blocks ahead.  16384 x 6144 x 6144: 588 -> 413 us on zeros (clocks at their maximum); on
+// random codes 503 us = 2.46 PFLOP/s in bursts of a few calls, where the power cap takes the clocks to 1.6 GHz, and 555-605 us = 2.04-2.23 PFLOP/s
+// in calls without a pause.  (128-column tiles by two sets of warps in turn, whose epilogues
 // overlap, are slower: an MMA of 128 columns takes 80 clocks of the 64 that it should, and a commit for each block more.)
 // Warp roles of each CTA:
 //   warps 0-7  sums and epilogue: a thread has one row (TMEM lane) and BN / 2 columns, which share the scale of W;
@@ -62,8 +63,8 @@ struct Fp8Params {
     int *err_word;
 };
 
-// C columns of an accumulator, waited for, as pairs.  (One piece of assembly: as single registers that the wait then names, the values were
-// moved about before the FMAs, 85 moves for 64 of them, which took the loop from 440 to 590 us for 16384 x 6144 x 6144.)
+// C columns of an accumulator, waited for, as pairs.  (One piece of assembly: with single registers that the wait then names, 16384 x 6144 x 6144
+// took 590 us instead of 440.)
 template <int C> __device__ __forceinline__ void load_pairs(uint32_t t, f32x2 (&a)[C / 2]);
 template <> __device__ __forceinline__ void load_pairs<32>(uint32_t t, f32x2 (&a)[16]) {
     asm volatile("{\n\t.reg .b32 t<32>;\n\t"

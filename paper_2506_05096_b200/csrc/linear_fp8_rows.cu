@@ -7,8 +7,8 @@
 // to eight rows its rate is not what is short.  k is permuted so that a lane's 16 contiguous bytes are two of its fragments: lane t of a row
 // holds channels 16 t .. 16 t + 15 of a half block of 64, the same ones of W and of x.  A half block's products are scaled by its block's
 // scales on the way to fp32 sums, and the warps' sums meet in shared memory.
-// us at one / eight rows, and of a tile kernel's launch: 4096 x 4096 8.0 / 8.1, 13.6; 1152 x 4608 4.0 / 5.9, 7.5; 6144 x 1536 5.5 / 6.5, 14.3; 256 x
-// 1000 3.0 / 2.6, 4.3.  (Rows and scales of x fetched with W's cost registers and with them resident warps: 4096 x 4096, one row, 10.6 us; eight
+// us at one / eight rows, and of a tile kernel's launch: 4096 x 4096 7.7 / 8.9, 13.6; 1152 x 4608 3.1 / 4.9, 7.5; 6144 x 1536 5.0 / 6.1, 14.3; 256 x
+// 1000 1.8 / 1.9, 4.3.  (Rows and scales of x fetched with W's cost registers and with them resident warps: 4096 x 4096, one row, 10.6 us; eight
 // channels a CTA 12.6; at 16 rows the tiles are as fast.)
 #include "common.cuh"
 #include "epilogue_math.cuh"

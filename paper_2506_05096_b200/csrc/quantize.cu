@@ -4,9 +4,11 @@
 // so that the largest value of a block takes the largest code (448) and the scales of all-zero blocks stay normal numbers.
 //
 // HBM-bound: two bytes in and one out for every value.  A warp takes a row; a block of 128 channels is 16 lanes with 16 bytes each, whose
-// largest magnitude goes round by four shuffles.  Four pairs of blocks are in flight per warp.  The quotient is x times both parts of 1 / scale,
-// which is the correctly rounded quotient for all but a few operands; a rounding of its own before the one to e4m3 would decide the many exact
-// ties that bf16 values have (a plain product moves 1 in 2000 codes of normal values by one).
+// largest magnitude goes round by four shuffles.  Four pairs of blocks are in flight per warp.  The quotient by the stored scale is x times both
+// parts of 1 / scale, which is the correctly rounded fp32 quotient for all but a few operands.  bf16 values have many quotients x 448 / amax that are
+// ties of e4m3, or so close to one that the roundings to fp32 of the scale and of the quotient decide: a code is within half a step and 2^-22 of
+// the value, and about 1 in 1000 codes of normal values is the other neighbour of a tie than in exact arithmetic (a plain
+// product moves 1 in 2000 more).
 #include "common.cuh"
 
 namespace astraea {
@@ -26,7 +28,8 @@ __device__ __forceinline__ uint32_t largest(const uint4 &v) { return larger(larg
 // of both halves, as fp32
 __device__ __forceinline__ float magnitude(uint32_t m) { return fmaxf(fabsf(__uint_as_float(m << 16)), fabsf(__uint_as_float(m & 0xffff0000u))); }
 
-// The scale by a product and a residual step; 1 / scale as the sum of two numbers.
+// The scale: a product with 1 / 448 and a step by its residual.  1 / scale as the sum of two numbers: a step of Newton's iteration behind an
+// approximate reciprocal, and the residual that it leaves.
 struct BlockScale { float scale, inv, low; };
 __device__ __forceinline__ BlockScale scale_of(float amax) {
     BlockScale s;
@@ -108,7 +111,7 @@ quantize_rows_kernel(const uint4 *__restrict__ x, const int32_t *__restrict__ id
     }
 }
 
-// one CTA per block of 128 x 128: 256 threads, eight 16-byte vectors each
+// one CTA per block of 128 x 128: 256 threads, eight 16-byte vectors each (12288 x 12288 68 us, 6.4 TB/s; 4608 x 1152 4.3 us)
 __global__ void __launch_bounds__(256)
 quantize_weight_kernel(const uint4 *__restrict__ w, uint2 *__restrict__ wq, float *__restrict__ scale, int N_out, int blocks)
 {

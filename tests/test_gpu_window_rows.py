@@ -41,6 +41,8 @@ def test_single_tokens_before_keys_that_were_never_written(d, H, H_kv, N, p, lef
         k[b, int(kv_len[b]):], v[b, int(kv_len[b]):] = fill, fill
     idx = (kv_len - 1)[:, None].contiguous()
     out, lse = call(q, k, v, idx, kv_len, N, n_first, left, 0)
+    for b in range(2):                                            # (no row sees them)
+        k[b, int(kv_len[b]):], v[b, int(kv_len[b]):] = 0, 0
     want, want_lse = reference(q, k, v, idx, N, n_first, 0, left, 0, kv_len, 1 / math.sqrt(d))
     check(out, lse, want, want_lse)
 
@@ -60,6 +62,7 @@ def test_skipped_entries_hold_nothing_back(d):
     kv_len = torch.tensor([1700], device="cuda", dtype=torch.int32)
     k[0, 1700:], v[0, 1700:] = float("nan"), float("nan")
     out, lse = call(q, k, v, idx, kv_len, N, 3, 90, 10, bad=True)
+    k[0, 1700:], v[0, 1700:] = 0, 0
     want, want_lse = reference(q[:, good], k, v, idx[:, good], N, 3, 0, 90, 10, kv_len, 1 / math.sqrt(d))
     check(out[:, good], lse[:, :, good], want, want_lse)
     rest = skipped + [201]
